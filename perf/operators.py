@@ -135,7 +135,7 @@ def _code_of(ratio):
     """The code of a ratio weight / scale: nearest magnitude, a tie to the even index, no negative zero."""
     a = ratio.abs()
     index = (a > 0.25).to(torch.uint8) + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)
-    return index + 8 * ((ratio < 0) & (index > 0))
+    return index + ((ratio < 0) & (index > 0)).to(torch.uint8) * 8
 
 
 def _weights(case, g):
