@@ -54,7 +54,10 @@ extern "C" {
 
 typedef struct ssn_ctx ssn_ctx;
 
-typedef enum { SSN_F32 = 0, SSN_F64 = 1 } ssn_dtype;
+typedef enum {
+    SSN_F32 = 0, SSN_F64 = 1,
+    SSN_F16 = 2, SSN_BF16 = 3 /* only where a call below says so                                    */
+} ssn_dtype;
 typedef enum { SSN_DENSE_ROWMAJOR = 0, SSN_CSR = 1 } ssn_layout;
 typedef enum { SSN_SCALE_MEAN = 0, SSN_SCALE_SUM = 1 } ssn_scale;
 
@@ -300,6 +303,96 @@ int ssn_axpy(ssn_ctx *ctx, double alpha, const void *P, void *W_inout);
  * overlap on the same GPU (different streams, or threads) race; calls on one stream are safe. */
 #define SSN_STATIC_WORKSPACE_BYTES (48u << 20)
 int ssn_hessvec_static(const ssn_desc *d, const void *W, const int32_t *S, int64_t nS, const void *V, void *HV);
+
+/* ---- a softmax layer over many classes: log probabilities, their gradient, weights in 4 bits -------------------
+ * These calls need no context and allocate nothing: they check their arguments, enqueue kernels on a stream of the
+ * current device and return without waiting, so they may be recorded into a HIP graph.  Nothing is kept between calls;
+ * calls on different streams, and captured ones, need outputs and workspaces of their own. */
+
+/* Rows of margins z (the logits of a vocabulary's tokens, or X W), and what is asked of them.  Statistics ("type A") are
+ * float for SSN_F32, SSN_F16 and SSN_BF16 margins and double for SSN_F64; sums are formed in that type. */
+typedef struct {
+    int64_t n;                /* rows, 0 <= n < 2^31; 0: nothing is done, no pointer is looked at */
+    int64_t C;                /* classes, 1 <= C < 2^31                                          */
+    int32_t dtype;            /* of Z and dZ: any ssn_dtype                                      */
+    int32_t reference;        /* 0: Z has C columns; 1: Z has C - 1, and class C - 1 is the reference class, whose
+                                 margin is zero (C >= 2)                                         */
+    const void *Z;            /* [dev] n rows, element (i,c) at [i*ldz + c], aligned to an element; not NULL */
+    int64_t ldz;              /* >= the number of columns                                        */
+    const uint32_t *allowed;  /* [dev, nullable] class c of row i takes part iff bit c % 32 of word
+                                 [i*ld_allowed + c / 32] is set; NULL: every class               */
+    int64_t ld_allowed;       /* >= ceil(C / 32), or 0: one mask for all rows                    */
+    const int32_t *labels;    /* [dev] n x m given classes, row by row; a negative one is padding */
+    int32_t m;                /* 0 <= m <= 64 given classes per row                              */
+    int32_t k;                /* 0 <= k <= min(64, C) alternatives per row (ssn_logprobs)        */
+    void *stream;             /* hipStream_t, or NULL                                            */
+} ssn_rows;
+
+/* Log probabilities, entropy and the most probable classes of every row, from one pass over Z.  With M = max_c z_c over
+ * the allowed classes and L = log sum_c e^{z_c - M} (eq. (8), (9), M without the paper's lower bound of zero):
+ *   logp     [dev] n x m: (z_y - M) - L for the given classes y
+ *   maxpart  [dev, nullable] n: M            logpart [dev, nullable] n: L
+ *   entropy  [dev, nullable] n: -sum_c p_c log p_c
+ *   top_ids  [dev] n x k int32, top_logp [dev] n x k: the k largest margins in descending order, equal ones by ascending
+ *            class
+ * What is held at a class that is not allowed is not used; such a class counts as a margin of -inf.
+ *   - a class of margin -inf: log probability -inf, no share in the entropy, never among the alternatives: slots left
+ *     over hold class -1 and -inf.  Finite margins are margins, the type's lowest value too.
+ *   - a row without a class of more than -inf: M = -inf, L = 0, entropy 0, every log probability -inf.
+ *   - a row with NaN or +inf at an allowed class has no distribution: NaN in all its values, classes -1.
+ *   - a given class < 0 is padding: 0.  A given class >= C: NaN.
+ * logp may be NULL if m is 0, top_ids and top_logp if k is 0.  workspace [dev], 8-byte aligned, of at least the size that
+ * ssn_logprobs_workspace stores in *bytes for the same n, C, dtype, reference and k (often 0; then it may be NULL); only
+ * for the duration of the call's kernels.  Returns SSN_OK, SSN_E_INVALID_ARG, SSN_E_UNSUPPORTED (n, C, m or k too large),
+ * SSN_E_TOO_LARGE (workspace too small) or SSN_E_HIP. */
+int ssn_logprobs(const ssn_rows *rows, void *logp, void *maxpart, void *logpart, void *entropy, int32_t *top_ids,
+                 void *top_logp, void *workspace, int64_t workspace_bytes);
+int ssn_logprobs_workspace(const ssn_rows *rows, int64_t *bytes);
+
+/* The gradient of  sum_it dlogp_it logp_it + sum_i dlse_i (M_i + L_i) + sum_i dentropy_i entropy_i  with respect to Z:
+ *   dz_c = sum_t dlogp_t (1[c = y_t] - p_c) + dlse p_c - dentropy p_c (log p_c + entropy).
+ * Z, allowed and labels as in the forward call, logp, maxpart, logpart (and entropy if dentropy is given) its outputs;
+ * dlogp [dev] n x m (NULL if m is 0), dlse, dentropy [dev, nullable] n, all of type A.  dZ [dev] like Z, leading dimension lddz: every
+ * column of Z is written.  dZ may be Z itself (with lddz = ldz) and must not overlap it otherwise.
+ * Classes that are not allowed and rows without a class get 0; a padding label and a given class of log
+ * probability -inf contribute nothing; a row with NaN or +inf, or with a given class >= C, gets NaN at its allowed classes.  A class given
+ * twice counts twice.  Returns like ssn_logprobs. */
+int ssn_logprobs_grad(const ssn_rows *rows, const void *logp, const void *maxpart, const void *logpart, const void *entropy,
+                      const void *dlogp, const void *dlse, const void *dentropy, void *dZ, int64_t lddz);
+
+/* A p-by-K weight block in 4 bits.  Features are padded to blocks of 128 and classes to tiles of 16.  A code is a sign
+ * (bit 3) and a magnitude index (bits 0-2) into {0, 1/2, 1, 3/2, 2, 3, 4, 6}; a weight is its code's number times the
+ * bfloat16 scale of its class and group of `group` consecutive features.
+ *   packed [dev], 16-byte aligned, ceil(K/16) * ceil(p/128) * 1024 bytes: byte b of word j of lane 16 g + o (g, j < 4) of
+ *     tile t, block q is at ((t * ceil(p/128) + q) * 64 + 16 g + o) * 16 + 4 j + b and holds features
+ *     128 q + 32 j + 8 g + 2 b (low nibble) and the next one (high nibble) of class 16 t + o.
+ *   scales [dev], 8-byte aligned, ceil(K/16) * ceil(p/128) * 16 * (128/group) bfloat16 values: [t][q][o][group].
+ * What stands in the padding must be finite (ssn_q4_quantize writes zeros). */
+typedef struct {
+    int64_t p, K;             /* features, classes; each in [1, 2^31)                            */
+    int32_t group;            /* 32, 64 or 128 features to a scale                               */
+    int32_t reserved;         /* 0                                                               */
+    uint8_t *packed;          /* [dev]                                                           */
+    uint16_t *scales;         /* [dev]                                                           */
+} ssn_q4;
+
+/* Lays a weight block out in 4 bits: entry (j,c) of W is at W[j*stride_j + c*stride_c] (strides in elements, >= 1, no
+ * smaller one need be 1; the p-by-K blocks of this library: ldw and 1), of any ssn_dtype.  A scale is the smallest bfloat16
+ * number s with 6 s >= every magnitude of its group, so no weight is clipped; a code the magnitude nearest to |w| / s, a tie
+ * going to the even index.  A group with NaN, an infinity or a weight that no scale reaches gets the scale NaN.  A set-up
+ * step; asynchronous. */
+int ssn_q4_quantize(const ssn_q4 *block, int32_t dtype, const void *W, int64_t stride_j, int64_t stride_c, void *stream);
+
+/* Margins of rows of features with such a block: Z = X W, z_ic = sum_j x_ij w_jc.  X [dev] n rows of p elements, leading
+ * dimension ldx >= p, SSN_F32, SSN_F16 or SSN_BF16; Z [dev] n rows of K elements, leading dimension ldz >= K, of type
+ * zdtype: X's or SSN_F32; both aligned to an element.  Products are exact, sums in fp32, rounded once to Z's type; the
+ * order of the sums depends on the sizes only, also on n.  Z must not overlap X.  n = 0: nothing is done.  workspace [dev],
+ * 4-byte aligned, of at least the size that ssn_q4_margins_workspace stores in *bytes for the same sizes (often 0; then it
+ * may be NULL).  Returns SSN_OK, SSN_E_INVALID_ARG, SSN_E_UNSUPPORTED (n of 2^20 or more, SSN_F64), SSN_E_TOO_LARGE
+ * (workspace too small) or SSN_E_HIP. */
+int ssn_q4_margins(const ssn_q4 *block, int32_t dtype, int64_t n, const void *X, int64_t ldx, int32_t zdtype, void *Z,
+                   int64_t ldz, void *workspace, int64_t workspace_bytes, void *stream);
+int ssn_q4_margins_workspace(const ssn_q4 *block, int32_t dtype, int64_t n, int64_t *bytes);
 
 #ifdef __cplusplus
 }

@@ -6,13 +6,14 @@ been built (python -m paper_1802_09113_amd.build) importing this module's `lib()
 """
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libssn_hip.so")
 
-SSN_F32, SSN_F64 = 0, 1
+SSN_F32, SSN_F64, SSN_F16, SSN_BF16 = 0, 1, 2, 3
 SSN_DENSE_ROWMAJOR, SSN_CSR = 0, 1
 SSN_SCALE_MEAN, SSN_SCALE_SUM = 0, 1
 SSN_OK = 0
@@ -28,6 +29,8 @@ EXPORTS = [
     "ssn_gradient", "ssn_gradient_sampled", "ssn_hess_prepare", "ssn_hess_apply", "ssn_hessvec", "ssn_cg", "ssn_linesearch",
     "ssn_predict", "ssn_solve", "ssn_axpy", "ssn_normalize_columns", "ssn_objective_dev", "ssn_gradient_dev",
     "ssn_accuracy", "ssn_vec_to_rowmajor", "ssn_rowmajor_to_vec", "ssn_hessvec_static",
+    "ssn_logprobs", "ssn_logprobs_workspace", "ssn_logprobs_grad", "ssn_q4_quantize", "ssn_q4_margins",
+    "ssn_q4_margins_workspace",
 ]
 BENCH_EXPORTS = ["ssn_time_kernel", "ssn_dense_path", "ssn_sampled_slices", "ssn_direction_form"]          # include/ssn_bench.h
 
@@ -68,6 +71,19 @@ class ssn_iter_record(ctypes.Structure):
         ("ms_linesearch", ctypes.c_double), ("ms_update", ctypes.c_double),
         ("cg_iters", ctypes.c_int32), ("ls_evals", ctypes.c_int32), ("ls_ok", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
+
+
+class ssn_rows(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int64), ("C", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reference", ctypes.c_int32),
+        ("Z", ctypes.c_void_p), ("ldz", ctypes.c_int64), ("allowed", ctypes.c_void_p), ("ld_allowed", ctypes.c_int64),
+        ("labels", ctypes.c_void_p), ("m", ctypes.c_int32), ("k", ctypes.c_int32), ("stream", ctypes.c_void_p),
+    ]
+
+
+class ssn_q4(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_int64), ("K", ctypes.c_int64), ("group", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("packed", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
 _lib = None
@@ -112,6 +128,14 @@ def lib():
         L.ssn_vec_to_rowmajor.argtypes = [vp, vp, vp]
         L.ssn_rowmajor_to_vec.argtypes = [vp, vp, vp]
         L.ssn_hessvec_static.argtypes = [ctypes.POINTER(ssn_desc), vp, vp, ctypes.c_int64, vp, vp]
+        i32, i64, lp, rows, q4 = (ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ssn_rows),
+                                  ctypes.POINTER(ssn_q4))
+        L.ssn_logprobs.argtypes = [rows, vp, vp, vp, vp, vp, vp, vp, i64]
+        L.ssn_logprobs_workspace.argtypes = [rows, lp]
+        L.ssn_logprobs_grad.argtypes = [rows, vp, vp, vp, vp, vp, vp, vp, vp, i64]
+        L.ssn_q4_quantize.argtypes = [q4, i32, vp, i64, i64, vp]
+        L.ssn_q4_margins.argtypes = [q4, i32, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+        L.ssn_q4_margins_workspace.argtypes = [q4, i32, i64, lp]
         for name in EXPORTS + BENCH_EXPORTS:
             fn = getattr(L, name)
             if fn.restype is not ctypes.c_char_p:
@@ -358,3 +382,169 @@ class Context:
         fields = [f[0] for f in ssn_iter_record._fields_ if f[0] != "reserved"]
         nrec = min(done.value + 1, int(pr.iters))
         return [{k: getattr(log[i], k) for k in fields} for i in range(nrec)], done.value
+
+
+# ---- a softmax layer over many classes -----------------------------------------------------------------------------
+
+_DTYPE = {torch.float32: SSN_F32, torch.float64: SSN_F64, torch.float16: SSN_F16, torch.bfloat16: SSN_BF16}
+
+
+def _at(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _ld(t):
+    """Leading dimension of a matrix whose rows are contiguous (the stride of a single row means nothing)."""
+    n, width = t.shape
+    assert width == 1 or t.stride(1) == 1, "rows must be contiguous"
+    return t.stride(0) if n > 1 else width
+
+
+def _stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _on_device(fn):
+    """Calls fn with the device of its first tensor current: kernels go to that device's current stream."""
+    def call(first, *args, **kw):
+        t = first.packed if isinstance(first, Q4Block) else first
+        assert t.is_cuda
+        if t.device.index == torch.cuda.current_device():
+            return fn(first, *args, **kw)
+        with torch.cuda.device(t.device):
+            return fn(first, *args, **kw)
+    call.__name__, call.__doc__ = fn.__name__, fn.__doc__
+    return call
+
+
+def _rows(Z, labels, k, reference, allowed):
+    assert Z.dim() == 2
+    n, width = Z.shape
+    d = ssn_rows(n, width + bool(reference), _DTYPE[Z.dtype], bool(reference), Z.data_ptr(), _ld(Z), None, 0, None, 0, k,
+                 _stream(Z.device))
+    if allowed is not None:
+        words = (d.C + 31) // 32
+        assert allowed.device == Z.device and allowed.dtype == torch.int32 and allowed.shape[-1] == words
+        assert allowed.stride(-1) == 1 or words == 1
+        assert allowed.dim() == 1 or (allowed.dim() == 2 and allowed.shape[0] == n)
+        d.allowed = allowed.data_ptr()
+        d.ld_allowed = 0 if allowed.dim() == 1 else allowed.stride(0) if n > 1 else words
+    if labels is not None:
+        assert labels.device == Z.device and labels.dtype == torch.int32 and labels.is_contiguous()
+        assert labels.shape[0] == n and labels.dim() <= 2
+        d.labels, d.m = labels.data_ptr(), labels.shape[1] if labels.dim() == 2 else 1
+    return d
+
+
+def _stat(t, like, shape):
+    """A contiguous tensor of statistics (float64 for float64 margins, float32 for the others), or None."""
+    assert t is None or (t.device == like.device and t.is_contiguous() and t.numel() == shape
+                         and t.dtype == (torch.float64 if like.dtype == torch.float64 else torch.float32))
+    return _at(t)
+
+
+@_on_device
+def ssn_logprobs(Z, labels=None, k=0, reference=False, allowed=None, out=None):
+    """Log probabilities of given classes, entropy and the k most probable classes of rows of margins.
+
+    Z: n x C device tensor (float32, float64, float16, bfloat16), rows contiguous; with reference=True n x (C - 1), and
+    class C - 1 has margin zero.  labels: int32, (n,) or (n, m), negative = padding.  allowed: int32 words of bits, (n,
+    ceil(C / 32)) or one row of words for all.  Returns a dict of logp (shaped like labels), maxpart, logpart, entropy
+    and, with k > 0, top_ids and top_logp; `out` may bring any of them (missing or None: entropy, maxpart and logpart are
+    then not computed, the others allocated)."""
+    d = _rows(Z, labels, k, reference, allowed)
+    n, dev, stat = Z.shape[0], Z.device, torch.float64 if Z.dtype == torch.float64 else torch.float32
+    if out is None:
+        out = {name: torch.empty(n, dtype=stat, device=dev) for name in ("maxpart", "logpart", "entropy")}
+    if labels is not None and out.get("logp") is None:
+        out["logp"] = torch.empty(labels.shape, dtype=stat, device=dev)
+    if k and out.get("top_ids") is None:
+        out["top_ids"] = torch.empty((n, k), dtype=torch.int32, device=dev)
+    if k and out.get("top_logp") is None:
+        out["top_logp"] = torch.empty((n, k), dtype=stat, device=dev)
+    ids = out.get("top_ids")
+    assert not k or (ids.device == dev and ids.dtype == torch.int32 and ids.is_contiguous() and ids.numel() == n * k)
+    size = ctypes.c_int64()
+    L = lib()
+    st = L.ssn_logprobs_workspace(ctypes.byref(d), ctypes.byref(size))
+    if st == SSN_OK:
+        work = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
+        st = L.ssn_logprobs(ctypes.byref(d), _stat(out.get("logp"), Z, n * d.m) if d.m else None,
+                            _stat(out.get("maxpart"), Z, n), _stat(out.get("logpart"), Z, n), _stat(out.get("entropy"), Z, n),
+                            _at(ids) if k else None, _stat(out.get("top_logp"), Z, n * k) if k else None, _at(work), size.value)
+    if st != SSN_OK:
+        raise SsnError(st, "in ssn_logprobs")
+    return out
+
+
+@_on_device
+def ssn_logprobs_grad(Z, labels, forward, dlogp=None, dlse=None, dentropy=None, reference=False, allowed=None, dZ=None):
+    """The gradient with respect to Z of sum dlogp * logp + sum dlse * (maxpart + logpart) + sum dentropy * entropy; forward
+    is what ssn_logprobs returned for Z, labels, reference and allowed.  dZ: like Z, or Z itself."""
+    d = _rows(Z, labels, 0, reference, allowed)
+    n = Z.shape[0]
+    dZ = torch.empty(Z.shape, dtype=Z.dtype, device=Z.device) if dZ is None else dZ
+    assert dZ.device == Z.device and dZ.dtype == Z.dtype and dZ.shape == Z.shape
+    st = lib().ssn_logprobs_grad(ctypes.byref(d), _stat(forward["logp"], Z, n * d.m) if d.m else None,
+                                 _stat(forward["maxpart"], Z, n), _stat(forward["logpart"], Z, n),
+                                 _stat(forward["entropy"], Z, n) if dentropy is not None else None, _stat(dlogp, Z, n * d.m),
+                                 _stat(dlse, Z, n), _stat(dentropy, Z, n), dZ.data_ptr(), _ld(dZ))
+    if st != SSN_OK:
+        raise SsnError(st, "in ssn_logprobs_grad")
+    return dZ
+
+
+class Q4Block(NamedTuple):
+    """A p x K weight block in 4 bits (ssn_q4 of ssn.h): packed uint8, scales bfloat16, both contiguous device tensors."""
+    packed: torch.Tensor
+    scales: torch.Tensor
+    p: int
+    K: int
+    group: int
+
+
+def _q4(block):
+    packed, scales, p, K, group = block
+    tiles = -(-K // 16) * -(-p // 128)
+    assert packed.dtype == torch.uint8 and scales.dtype == torch.bfloat16 and scales.device == packed.device
+    assert packed.is_contiguous() and packed.numel() == tiles * 1024
+    assert scales.is_contiguous() and scales.numel() * group == tiles * 2048
+    return ssn_q4(p, K, group, 0, packed.data_ptr(), scales.data_ptr())
+
+
+@_on_device
+def ssn_q4_quantize(W, group=32):
+    """A p x K weight block (any strides, float32 / float64 / float16 / bfloat16; a K x p layer as its transpose) in 4 bits,
+    one scale for each class and `group` features."""
+    assert W.dim() == 2
+    (p, K), (sj, sc) = W.shape, W.stride()
+    tiles, blocks = -(-K // 16), -(-p // 128)
+    assert group in (32, 64, 128)
+    block = Q4Block(torch.empty((tiles, blocks, 64, 16), dtype=torch.uint8, device=W.device),
+                    torch.empty((tiles, blocks, 16, 128 // group), dtype=torch.bfloat16, device=W.device), p, K, group)
+    d = _q4(block)
+    st = lib().ssn_q4_quantize(ctypes.byref(d), _DTYPE[W.dtype], W.data_ptr(), sj if p > 1 else 1, sc if K > 1 else 1,
+                               _stream(W.device))
+    if st != SSN_OK:
+        raise SsnError(st, "in ssn_q4_quantize")
+    return block
+
+
+@_on_device
+def ssn_q4_margins(block, X, Z=None):
+    """Margins X W of n x p rows (float32, float16, bfloat16; rows contiguous) with a block in 4 bits: n x K, of X's type
+    unless a float32 Z is given."""
+    d = _q4(block)
+    assert X.dim() == 2 and X.device == block.packed.device and X.shape[1] == block.p
+    n = X.shape[0]
+    Z = torch.empty((n, block.K), dtype=X.dtype, device=X.device) if Z is None else Z
+    assert Z.device == X.device and Z.shape == (n, block.K)
+    L, size, dt = lib(), ctypes.c_int64(), _DTYPE[X.dtype]
+    st = L.ssn_q4_margins_workspace(ctypes.byref(d), dt, n, ctypes.byref(size))
+    if st == SSN_OK:
+        work = torch.empty(size.value, dtype=torch.uint8, device=X.device) if size.value else None
+        st = L.ssn_q4_margins(ctypes.byref(d), dt, n, X.data_ptr(), _ld(X), _DTYPE[Z.dtype], Z.data_ptr(), _ld(Z), _at(work),
+                              size.value, _stream(X.device))
+    if st != SSN_OK:
+        raise SsnError(st, "in ssn_q4_margins")
+    return Z

@@ -4,6 +4,7 @@
 #include "ssn_internal.h"
 #include "ssn_bench.h"
 
+#include <atomic>
 #include <chrono>
 #include <cmath>
 #include <cstddef>
@@ -2085,6 +2086,192 @@ int ssn_dense_path(const ssn_ctx *c)
     if (!is_dense(c)) return 0;
     if (c->binary) return 3;
     return c->fused ? 2 : 1;
+}
+
+}  // extern "C"
+
+// ---- a softmax layer over many classes (logprobs.hip, q4.hip) ----------------------------------------------
+namespace {
+std::atomic<int> device_cus[STATIC_MAX_DEVICES];
+
+// compute units of the current device
+int current_cus(int *cus)
+{
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= STATIC_MAX_DEVICES) return SSN_E_HIP;
+    int c = device_cus[dev].load(std::memory_order_relaxed);
+    if (!c) {
+        if (hipDeviceGetAttribute(&c, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || c < 1) return SSN_E_HIP;
+        device_cus[dev].store(c, std::memory_order_relaxed);
+    }
+    *cus = c;
+    return SSN_OK;
+}
+
+int elem_size(int32_t dtype) { return dtype == SSN_F64 ? 8 : dtype == SSN_F32 ? 4 : dtype == SSN_F16 || dtype == SSN_BF16 ? 2 : 0; }
+bool aligned_to(const void *q, size_t bytes) { return ((uintptr_t)q & (bytes - 1)) == 0; }
+
+// the sizes of an ssn_rows
+int rows_sizes(const ssn_rows *r, LogprobsArgs *a)
+{
+    if (!r || r->n < 0 || !elem_size(r->dtype) || (r->reference != 0 && r->reference != 1)) return SSN_E_INVALID_ARG;
+    if (r->C < 1 + r->reference || r->m < 0 || r->k < 0) return SSN_E_INVALID_ARG;
+    if (r->C >= (int64_t)1 << 31 || r->n >= (int64_t)1 << 31 || r->m > LOGPROBS_MAX_GIVEN || r->k > LOGPROBS_MAX_TOP)
+        return SSN_E_UNSUPPORTED;
+    if (r->k > r->C) return SSN_E_INVALID_ARG;
+    *a = LogprobsArgs{};
+    a->n = r->n;
+    a->C = r->C;
+    a->width = r->C - r->reference;
+    a->m = r->m;
+    a->k = r->k;
+    a->reference = r->reference;
+    return SSN_OK;
+}
+int rows_data(const ssn_rows *r, LogprobsArgs *a)
+{
+    SSN_TRY(rows_sizes(r, a));
+    if (!a->n) return SSN_OK;
+    if (!r->Z || r->ldz < a->width || !aligned_to(r->Z, elem_size(r->dtype)) || (r->m && !r->labels)) return SSN_E_INVALID_ARG;
+    if (r->allowed && r->ld_allowed != 0 && r->ld_allowed < (r->C + 31) / 32) return SSN_E_INVALID_ARG;
+    a->Z = r->Z;
+    a->ldz = r->ldz;
+    a->allowed = r->allowed;
+    a->ld_allowed = r->ld_allowed;
+    a->labels = r->labels;
+    return SSN_OK;
+}
+
+int q4_sizes(const ssn_q4 *b, Q4Args *a)
+{
+    if (!b || b->p < 1 || b->K < 1 || (b->group != 32 && b->group != 64 && b->group != 128) || b->reserved) return SSN_E_INVALID_ARG;
+    if (b->p >= (int64_t)1 << 31 || b->K >= (int64_t)1 << 31) return SSN_E_UNSUPPORTED;
+    *a = Q4Args{};
+    a->p = b->p;
+    a->K = b->K;
+    a->group = b->group;
+    return SSN_OK;
+}
+int q4_rows(const ssn_q4 *b, int32_t dtype, int64_t n, Q4Args *a)
+{
+    SSN_TRY(q4_sizes(b, a));
+    if (n < 0 || !elem_size(dtype)) return SSN_E_INVALID_ARG;
+    if (dtype == SSN_F64 || n >= (int64_t)1 << 20) return SSN_E_UNSUPPORTED;
+    a->dtype = dtype;
+    a->n = n;
+    return SSN_OK;
+}
+int q4_parts(Q4Args *a)
+{
+    int cus = 0;
+    SSN_TRY(current_cus(&cus));
+    q4_plan(cus, a);
+    return SSN_OK;
+}
+}  // namespace
+
+extern "C" {
+
+int ssn_logprobs_workspace(const ssn_rows *r, int64_t *bytes)
+{
+    if (!bytes) return SSN_E_INVALID_ARG;
+    LogprobsArgs a;
+    SSN_TRY(rows_sizes(r, &a));
+    *bytes = 0;
+    if (!a.n) return SSN_OK;
+    int cus = 0;
+    SSN_TRY(current_cus(&cus));
+    logprobs_plan(r->dtype, a.n, a.C, a.width, a.k, cus, &a);
+    *bytes = logprobs_workspace(r->dtype, a.n, a.k, a);
+    return SSN_OK;
+}
+
+int ssn_logprobs(const ssn_rows *r, void *logp, void *maxpart, void *logpart, void *entropy, int32_t *top_ids, void *top_logp,
+                 void *workspace, int64_t workspace_bytes)
+{
+    LogprobsArgs a;
+    SSN_TRY(rows_data(r, &a));
+    if (!a.n) return SSN_OK;
+    if ((a.m && !logp) || (a.k && (!top_ids || !top_logp))) return SSN_E_INVALID_ARG;
+    a.logp = logp;
+    a.maxpart = maxpart;
+    a.logpart = logpart;
+    a.entropy = entropy;
+    a.top_ids = top_ids;
+    a.top_logp = top_logp;
+    int cus = 0;
+    SSN_TRY(current_cus(&cus));
+    logprobs_plan(r->dtype, a.n, a.C, a.width, a.k, cus, &a);
+    const int64_t need = logprobs_workspace(r->dtype, a.n, a.k, a);
+    if (need > 0 && (!workspace || !aligned_to(workspace, 8))) return SSN_E_INVALID_ARG;
+    if (need > workspace_bytes) return SSN_E_TOO_LARGE;
+    return launch_logprobs(r->dtype, a, workspace, (hipStream_t)r->stream) == hipSuccess ? SSN_OK : SSN_E_HIP;
+}
+
+int ssn_logprobs_grad(const ssn_rows *r, const void *logp, const void *maxpart, const void *logpart, const void *entropy,
+                      const void *dlogp, const void *dlse, const void *dentropy, void *dZ, int64_t lddz)
+{
+    LogprobsArgs a;
+    SSN_TRY(rows_data(r, &a));
+    if (!a.n) return SSN_OK;
+    if (!maxpart || !logpart || !dZ || lddz < a.width || !aligned_to(dZ, elem_size(r->dtype))) return SSN_E_INVALID_ARG;
+    if ((a.m && (!logp || !dlogp)) || (dentropy && !entropy) || (dZ == r->Z && lddz != r->ldz)) return SSN_E_INVALID_ARG;
+    a.logp = const_cast<void *>(logp);
+    a.maxpart = const_cast<void *>(maxpart);
+    a.logpart = const_cast<void *>(logpart);
+    a.entropy = const_cast<void *>(entropy);
+    a.dlogp = dlogp;
+    a.dlse = dlse;
+    a.dentropy = dentropy;
+    a.dZ = dZ;
+    a.lddz = lddz;
+    return launch_logprobs_grad(r->dtype, a, (hipStream_t)r->stream) == hipSuccess ? SSN_OK : SSN_E_HIP;
+}
+
+int ssn_q4_quantize(const ssn_q4 *b, int32_t dtype, const void *W, int64_t stride_j, int64_t stride_c, void *stream)
+{
+    Q4Args a;
+    SSN_TRY(q4_sizes(b, &a));
+    if (!elem_size(dtype) || !W || !aligned_to(W, elem_size(dtype)) || stride_j < 1 || stride_c < 1) return SSN_E_INVALID_ARG;
+    if (!b->packed || !b->scales || !aligned_to(b->packed, 16) || !aligned_to(b->scales, 8)) return SSN_E_INVALID_ARG;
+    return launch_q4_quantize(dtype, a.p, a.K, W, stride_j, stride_c, a.group, b->packed, b->scales, (hipStream_t)stream) == hipSuccess
+               ? SSN_OK
+               : SSN_E_HIP;
+}
+
+int ssn_q4_margins_workspace(const ssn_q4 *b, int32_t dtype, int64_t n, int64_t *bytes)
+{
+    if (!bytes) return SSN_E_INVALID_ARG;
+    Q4Args a;
+    SSN_TRY(q4_rows(b, dtype, n, &a));
+    *bytes = 0;
+    if (!n) return SSN_OK;
+    SSN_TRY(q4_parts(&a));
+    *bytes = q4_workspace(a);
+    return SSN_OK;
+}
+
+int ssn_q4_margins(const ssn_q4 *b, int32_t dtype, int64_t n, const void *X, int64_t ldx, int32_t zdtype, void *Z, int64_t ldz,
+                   void *workspace, int64_t workspace_bytes, void *stream)
+{
+    Q4Args a;
+    SSN_TRY(q4_rows(b, dtype, n, &a));
+    if (!n) return SSN_OK;
+    if (!b->packed || !b->scales || !aligned_to(b->packed, 16) || !aligned_to(b->scales, 8)) return SSN_E_INVALID_ARG;
+    if (!X || !Z || ldx < a.p || ldz < a.K || (zdtype != dtype && zdtype != SSN_F32)) return SSN_E_INVALID_ARG;
+    if (!aligned_to(X, elem_size(dtype)) || !aligned_to(Z, elem_size(zdtype))) return SSN_E_INVALID_ARG;
+    a.packed = b->packed;
+    a.scales = b->scales;
+    a.X = X;
+    a.ldx = ldx;
+    a.Z = Z;
+    a.ldz = ldz;
+    a.zdtype = zdtype;
+    SSN_TRY(q4_parts(&a));
+    const int64_t need = q4_workspace(a);
+    if (need > 0 && (!workspace || !aligned_to(workspace, 4))) return SSN_E_INVALID_ARG;
+    if (need > workspace_bytes) return SSN_E_TOO_LARGE;
+    return launch_q4_margins(a, workspace, (hipStream_t)stream) == hipSuccess ? SSN_OK : SSN_E_HIP;
 }
 
 }  // extern "C"

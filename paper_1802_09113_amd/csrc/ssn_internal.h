@@ -475,4 +475,53 @@ struct HessCg {
 // r: the sample's rows (S, nrows) and the row stride KP of their probabilities P
 hipError_t launch_hess_small(int dtype, const HessSmall &h, const RowsArgs &r, const void *P, double *part, HessCg a, hipStream_t st);
 
+// ---- log probabilities of rows of margins, and their gradient (logprobs.hip) -------------------------------
+struct LogprobsArgs {
+    int64_t n, C, width;     // rows, classes, columns of Z (C, or C - 1 with the reference class)
+    const void *Z;
+    int64_t ldz;
+    const uint32_t *allowed; // nullable: bit c % 32 of word c / 32 of the row; ld_allowed words between rows
+    int64_t ld_allowed;
+    const int32_t *labels;   // n x m
+    int32_t m, k, reference;
+    void *logp, *maxpart, *logpart, *entropy;      // outputs of the forward call, inputs of the gradient
+    int32_t *top_ids;
+    void *top_logp;
+    const void *dlogp, *dlse, *dentropy;           // gradient only
+    void *dZ;
+    int64_t lddz;
+    // set by logprobs_plan: waves per workgroup (0: the form for few classes), workgroups per row, columns of a wave
+    int32_t waves, parts;
+    int64_t per_wave;
+    void *ws_stat, *ws_val;                        // set by the launcher: (M, s, t) and k alternatives of every part
+    int32_t *ws_id;
+};
+constexpr int LOGPROBS_MAX_GIVEN = 64, LOGPROBS_MAX_TOP = 64, LOGPROBS_MAX_PARTS = 64;     // a lane for each
+void logprobs_plan(int dtype, int64_t n, int64_t C, int64_t width, int k, int num_cus, LogprobsArgs *a);
+int64_t logprobs_workspace(int dtype, int64_t n, int k, const LogprobsArgs &a);
+hipError_t launch_logprobs(int dtype, LogprobsArgs &a, void *workspace, hipStream_t st);
+hipError_t launch_logprobs_grad(int dtype, const LogprobsArgs &a, hipStream_t st);
+
+// ---- margins with a weight block held in 4 bits (q4.hip) ----------------------------------------------------
+struct Q4Args {
+    int64_t p, K;
+    int32_t group;
+    const uint8_t *packed;
+    const uint16_t *scales;
+    int64_t n;
+    const void *X;
+    int64_t ldx;
+    void *Z;
+    int64_t ldz;
+    int32_t dtype, zdtype;
+    // set by q4_plan: parts of the features (partial sums of each in the workspace where there is more than one)
+    int32_t parts;
+    float *ws;
+};
+void q4_plan(int num_cus, Q4Args *a);
+int64_t q4_workspace(const Q4Args &a);
+hipError_t launch_q4_margins(Q4Args &a, void *workspace, hipStream_t st);
+hipError_t launch_q4_quantize(int dtype, int64_t p, int64_t K, const void *W, int64_t sj, int64_t sc, int group, uint8_t *packed,
+                              uint16_t *scales, hipStream_t st);
+
 }  // namespace ssn
