@@ -385,12 +385,12 @@ class Context:
 
 
 # ---- a softmax layer over many classes -----------------------------------------------------------------------------
+# The smallest of these calls are a kernel of a few microseconds: what the binding does around them is kept to plain
+# attribute reads (torch's own accessors of the current device and stream, one library call where no workspace is needed).
 
 _DTYPE = {torch.float32: SSN_F32, torch.float64: SSN_F64, torch.float16: SSN_F16, torch.bfloat16: SSN_BF16}
-
-
-def _at(t):
-    return t.data_ptr() if t is not None else None
+_STAT = {torch.float32: torch.float32, torch.float16: torch.float32, torch.bfloat16: torch.float32, torch.float64: torch.float64}
+_get_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _ld(t):
@@ -400,50 +400,40 @@ def _ld(t):
     return t.stride(0) if n > 1 else width
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+def _elsewhere(t):
+    """Whether t lives on another device than the current one (kernels go to its device's current stream)."""
+    assert t.is_cuda
+    return t.get_device() != _get_device()
 
 
-def _on_device(fn):
-    """Calls fn with the device of its first tensor current: kernels go to that device's current stream."""
-    def call(first, *args, **kw):
-        t = first.packed if isinstance(first, Q4Block) else first
-        assert t.is_cuda
-        if t.device.index == torch.cuda.current_device():
-            return fn(first, *args, **kw)
-        with torch.cuda.device(t.device):
-            return fn(first, *args, **kw)
-    call.__name__, call.__doc__ = fn.__name__, fn.__doc__
-    return call
-
-
-def _rows(Z, labels, k, reference, allowed):
-    assert Z.dim() == 2
+def _rows(Z, labels, k, reference, allowed, dev):
     n, width = Z.shape
-    d = ssn_rows(n, width + bool(reference), _DTYPE[Z.dtype], bool(reference), Z.data_ptr(), _ld(Z), None, 0, None, 0, k,
-                 _stream(Z.device))
+    reference = 1 if reference else 0
+    C = width + reference
+    at_allowed, ld_allowed, at_labels, m = None, 0, None, 0
     if allowed is not None:
-        words = (d.C + 31) // 32
-        assert allowed.device == Z.device and allowed.dtype == torch.int32 and allowed.shape[-1] == words
+        words = (C + 31) // 32
+        assert allowed.get_device() == dev and allowed.dtype is torch.int32 and allowed.shape[-1] == words
         assert allowed.stride(-1) == 1 or words == 1
         assert allowed.dim() == 1 or (allowed.dim() == 2 and allowed.shape[0] == n)
-        d.allowed = allowed.data_ptr()
-        d.ld_allowed = 0 if allowed.dim() == 1 else allowed.stride(0) if n > 1 else words
+        at_allowed, ld_allowed = allowed.data_ptr(), 0 if allowed.dim() == 1 else allowed.stride(0) if n > 1 else words
     if labels is not None:
-        assert labels.device == Z.device and labels.dtype == torch.int32 and labels.is_contiguous()
-        assert labels.shape[0] == n and labels.dim() <= 2
-        d.labels, d.m = labels.data_ptr(), labels.shape[1] if labels.dim() == 2 else 1
-    return d
+        assert labels.get_device() == dev and labels.dtype is torch.int32 and labels.is_contiguous()
+        shape = labels.shape
+        assert shape[0] == n and len(shape) <= 2
+        at_labels, m = labels.data_ptr(), shape[1] if len(shape) == 2 else 1
+    return ssn_rows(n, C, _DTYPE[Z.dtype], reference, Z.data_ptr(), _ld(Z), at_allowed, ld_allowed, at_labels, m, k,
+                    _raw_stream(dev)), n, m
 
 
-def _stat(t, like, shape):
-    """A contiguous tensor of statistics (float64 for float64 margins, float32 for the others), or None."""
-    assert t is None or (t.device == like.device and t.is_contiguous() and t.numel() == shape
-                         and t.dtype == (torch.float64 if like.dtype == torch.float64 else torch.float32))
-    return _at(t)
+def _data(t, dtype, count, dev):
+    """The address of a contiguous tensor of `count` elements, or None."""
+    if t is None:
+        return None
+    assert t.dtype is dtype and t.numel() == count and t.get_device() == dev and t.is_contiguous()
+    return t.data_ptr()
 
 
-@_on_device
 def ssn_logprobs(Z, labels=None, k=0, reference=False, allowed=None, out=None):
     """Log probabilities of given classes, entropy and the k most probable classes of rows of margins.
 
@@ -452,43 +442,52 @@ def ssn_logprobs(Z, labels=None, k=0, reference=False, allowed=None, out=None):
     ceil(C / 32)) or one row of words for all.  Returns a dict of logp (shaped like labels), maxpart, logpart, entropy
     and, with k > 0, top_ids and top_logp; `out` may bring any of them (missing or None: entropy, maxpart and logpart are
     then not computed, the others allocated)."""
-    d = _rows(Z, labels, k, reference, allowed)
-    n, dev, stat = Z.shape[0], Z.device, torch.float64 if Z.dtype == torch.float64 else torch.float32
+    if _elsewhere(Z):
+        with torch.cuda.device(Z.device):
+            return ssn_logprobs(Z, labels, k, reference, allowed, out)
+    dev, stat = Z.get_device(), _STAT[Z.dtype]
+    d, n, m = _rows(Z, labels, k, reference, allowed, dev)
     if out is None:
-        out = {name: torch.empty(n, dtype=stat, device=dev) for name in ("maxpart", "logpart", "entropy")}
-    if labels is not None and out.get("logp") is None:
-        out["logp"] = torch.empty(labels.shape, dtype=stat, device=dev)
-    if k and out.get("top_ids") is None:
-        out["top_ids"] = torch.empty((n, k), dtype=torch.int32, device=dev)
-    if k and out.get("top_logp") is None:
-        out["top_logp"] = torch.empty((n, k), dtype=stat, device=dev)
-    ids = out.get("top_ids")
-    assert not k or (ids.device == dev and ids.dtype == torch.int32 and ids.is_contiguous() and ids.numel() == n * k)
-    size = ctypes.c_int64()
+        out = {name: torch.empty(n, dtype=stat, device=Z.device) for name in ("maxpart", "logpart", "entropy")}
+    get = out.get
+    if labels is not None and get("logp") is None:
+        out["logp"] = torch.empty(labels.shape, dtype=stat, device=Z.device)
+    if k and get("top_ids") is None:
+        out["top_ids"] = torch.empty((n, k), dtype=torch.int32, device=Z.device)
+    if k and get("top_logp") is None:
+        out["top_logp"] = torch.empty((n, k), dtype=stat, device=Z.device)
+    args = (ctypes.byref(d), _data(out["logp"], stat, n * m, dev) if m else None, _data(get("maxpart"), stat, n, dev),
+            _data(get("logpart"), stat, n, dev), _data(get("entropy"), stat, n, dev),
+            _data(out["top_ids"], torch.int32, n * k, dev) if k else None,
+            _data(out["top_logp"], stat, n * k, dev) if k else None)
     L = lib()
-    st = L.ssn_logprobs_workspace(ctypes.byref(d), ctypes.byref(size))
-    if st == SSN_OK:
-        work = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
-        st = L.ssn_logprobs(ctypes.byref(d), _stat(out.get("logp"), Z, n * d.m) if d.m else None,
-                            _stat(out.get("maxpart"), Z, n), _stat(out.get("logpart"), Z, n), _stat(out.get("entropy"), Z, n),
-                            _at(ids) if k else None, _stat(out.get("top_logp"), Z, n * k) if k else None, _at(work), size.value)
+    st = L.ssn_logprobs(*args, None, 0)
+    if st == SSN_E_TOO_LARGE:                       # rows split over workgroups
+        size = ctypes.c_int64()
+        st = L.ssn_logprobs_workspace(args[0], ctypes.byref(size))
+        if st == SSN_OK:
+            work = torch.empty(size.value, dtype=torch.uint8, device=Z.device)
+            st = L.ssn_logprobs(*args, work.data_ptr(), size.value)
     if st != SSN_OK:
         raise SsnError(st, "in ssn_logprobs")
     return out
 
 
-@_on_device
 def ssn_logprobs_grad(Z, labels, forward, dlogp=None, dlse=None, dentropy=None, reference=False, allowed=None, dZ=None):
     """The gradient with respect to Z of sum dlogp * logp + sum dlse * (maxpart + logpart) + sum dentropy * entropy; forward
     is what ssn_logprobs returned for Z, labels, reference and allowed.  dZ: like Z, or Z itself."""
-    d = _rows(Z, labels, 0, reference, allowed)
-    n = Z.shape[0]
-    dZ = torch.empty(Z.shape, dtype=Z.dtype, device=Z.device) if dZ is None else dZ
-    assert dZ.device == Z.device and dZ.dtype == Z.dtype and dZ.shape == Z.shape
-    st = lib().ssn_logprobs_grad(ctypes.byref(d), _stat(forward["logp"], Z, n * d.m) if d.m else None,
-                                 _stat(forward["maxpart"], Z, n), _stat(forward["logpart"], Z, n),
-                                 _stat(forward["entropy"], Z, n) if dentropy is not None else None, _stat(dlogp, Z, n * d.m),
-                                 _stat(dlse, Z, n), _stat(dentropy, Z, n), dZ.data_ptr(), _ld(dZ))
+    if _elsewhere(Z):
+        with torch.cuda.device(Z.device):
+            return ssn_logprobs_grad(Z, labels, forward, dlogp, dlse, dentropy, reference, allowed, dZ)
+    dev, stat = Z.get_device(), _STAT[Z.dtype]
+    d, n, m = _rows(Z, labels, 0, reference, allowed, dev)
+    if dZ is None:
+        dZ = torch.empty(Z.shape, dtype=Z.dtype, device=Z.device)
+    assert dZ.get_device() == dev and dZ.dtype is Z.dtype and dZ.shape == Z.shape
+    st = lib().ssn_logprobs_grad(
+        ctypes.byref(d), _data(forward["logp"], stat, n * m, dev) if m else None, _data(forward["maxpart"], stat, n, dev),
+        _data(forward["logpart"], stat, n, dev), _data(forward["entropy"], stat, n, dev) if dentropy is not None else None,
+        _data(dlogp, stat, n * m, dev), _data(dlse, stat, n, dev), _data(dentropy, stat, n, dev), dZ.data_ptr(), _ld(dZ))
     if st != SSN_OK:
         raise SsnError(st, "in ssn_logprobs_grad")
     return dZ
@@ -503,48 +502,55 @@ class Q4Block(NamedTuple):
     group: int
 
 
-def _q4(block):
+def _q4(block, dev):
     packed, scales, p, K, group = block
     tiles = -(-K // 16) * -(-p // 128)
-    assert packed.dtype == torch.uint8 and scales.dtype == torch.bfloat16 and scales.device == packed.device
-    assert packed.is_contiguous() and packed.numel() == tiles * 1024
-    assert scales.is_contiguous() and scales.numel() * group == tiles * 2048
-    return ssn_q4(p, K, group, 0, packed.data_ptr(), scales.data_ptr())
+    assert group in (32, 64, 128)
+    return ssn_q4(p, K, group, 0, _data(packed, torch.uint8, tiles * 1024, dev), _data(scales, torch.bfloat16, tiles * 2048 // group, dev))
 
 
-@_on_device
 def ssn_q4_quantize(W, group=32):
     """A p x K weight block (any strides, float32 / float64 / float16 / bfloat16; a K x p layer as its transpose) in 4 bits,
     one scale for each class and `group` features."""
-    assert W.dim() == 2
+    if _elsewhere(W):
+        with torch.cuda.device(W.device):
+            return ssn_q4_quantize(W, group)
+    assert group in (32, 64, 128)
     (p, K), (sj, sc) = W.shape, W.stride()
     tiles, blocks = -(-K // 16), -(-p // 128)
-    assert group in (32, 64, 128)
     block = Q4Block(torch.empty((tiles, blocks, 64, 16), dtype=torch.uint8, device=W.device),
                     torch.empty((tiles, blocks, 16, 128 // group), dtype=torch.bfloat16, device=W.device), p, K, group)
-    d = _q4(block)
+    dev = W.get_device()
+    d = _q4(block, dev)
     st = lib().ssn_q4_quantize(ctypes.byref(d), _DTYPE[W.dtype], W.data_ptr(), sj if p > 1 else 1, sc if K > 1 else 1,
-                               _stream(W.device))
+                               _raw_stream(dev))
     if st != SSN_OK:
         raise SsnError(st, "in ssn_q4_quantize")
     return block
 
 
-@_on_device
 def ssn_q4_margins(block, X, Z=None):
     """Margins X W of n x p rows (float32, float16, bfloat16; rows contiguous) with a block in 4 bits: n x K, of X's type
     unless a float32 Z is given."""
-    d = _q4(block)
-    assert X.dim() == 2 and X.device == block.packed.device and X.shape[1] == block.p
-    n = X.shape[0]
-    Z = torch.empty((n, block.K), dtype=X.dtype, device=X.device) if Z is None else Z
-    assert Z.device == X.device and Z.shape == (n, block.K)
-    L, size, dt = lib(), ctypes.c_int64(), _DTYPE[X.dtype]
-    st = L.ssn_q4_margins_workspace(ctypes.byref(d), dt, n, ctypes.byref(size))
-    if st == SSN_OK:
-        work = torch.empty(size.value, dtype=torch.uint8, device=X.device) if size.value else None
-        st = L.ssn_q4_margins(ctypes.byref(d), dt, n, X.data_ptr(), _ld(X), _DTYPE[Z.dtype], Z.data_ptr(), _ld(Z), _at(work),
-                              size.value, _stream(X.device))
-    if st != SSN_OK:
-        raise SsnError(st, "in ssn_q4_margins")
+    if _elsewhere(X):
+        with torch.cuda.device(X.device):
+            return ssn_q4_margins(block, X, Z)
+    dev = X.get_device()
+    d = _q4(block, dev)
+    n, p = X.shape
+    assert p == d.p
+    if Z is None:
+        Z = torch.empty((n, d.K), dtype=X.dtype, device=X.device)
+    assert Z.get_device() == dev and Z.shape == (n, d.K)
+    dt, st, L = _DTYPE[X.dtype], _raw_stream(dev), lib()
+    args = (ctypes.byref(d), dt, n, X.data_ptr(), _ld(X), _DTYPE[Z.dtype], Z.data_ptr(), _ld(Z))
+    status = L.ssn_q4_margins(*args, None, 0, st)
+    if status == SSN_E_TOO_LARGE:                   # parts of the features, each with sums of its own
+        size = ctypes.c_int64()
+        status = L.ssn_q4_margins_workspace(args[0], dt, n, ctypes.byref(size))
+        if status == SSN_OK:
+            work = torch.empty(size.value, dtype=torch.uint8, device=X.device)
+            status = L.ssn_q4_margins(*args, work.data_ptr(), size.value, st)
+    if status != SSN_OK:
+        raise SsnError(status, "in ssn_q4_margins")
     return Z

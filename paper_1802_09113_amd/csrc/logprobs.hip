@@ -22,6 +22,18 @@ constexpr int NARROW_PER_LANE = 8;      // margins per lane of the narrow form
 template <typename T> struct Acc { typedef float type; };
 template <> struct Acc<double> { typedef double type; };
 
+// x where m is -1, -inf where m is 0
+__device__ __forceinline__ float keep_if(float x, int m)
+{
+    return __uint_as_float((__float_as_uint(x) & (uint32_t)m) | (0xff800000u & ~(uint32_t)m));
+}
+__device__ __forceinline__ double keep_if(double x, int m)
+{
+    const long long b = __double_as_longlong(x);
+    const uint32_t lo = (uint32_t)b & (uint32_t)m, hi = ((uint32_t)(b >> 32) & (uint32_t)m) | (0xfff00000u & ~(uint32_t)m);
+    return __longlong_as_double(((long long)hi << 32) | lo);
+}
+
 // 16 bytes of margins at an address aligned to an element only
 typedef uint32_t Raw __attribute__((ext_vector_type(4)));
 typedef Raw RawAt2 __attribute__((aligned(2)));
@@ -90,6 +102,15 @@ __device__ __forceinline__ float lowest(float) { return -__FLT_MAX__; }
 __device__ __forceinline__ double lowest(double) { return -__DBL_MAX__; }
 __device__ __forceinline__ float minus_inf(float) { return -__builtin_inff(); }
 __device__ __forceinline__ double minus_inf(double) { return -__builtin_inf(); }
+// -inf that the compiler does not know: it would keep a wave's constant of this value in a pair of scalar registers, and
+// writes it there with one instruction that holds only half of the number
+__device__ __forceinline__ float hidden_minus_inf(float) { return minus_inf(0.0f); }
+__device__ __forceinline__ double hidden_minus_inf(double)
+{
+    int hi = (int)0xfff00000;
+    asm volatile("" : "+v"(hi));
+    return __longlong_as_double((long long)hi << 32);
+}
 __device__ __forceinline__ float nan_of(float) { return __builtin_nanf(""); }
 __device__ __forceinline__ double nan_of(double) { return __builtin_nan(""); }
 
@@ -147,6 +168,22 @@ template <typename A> __device__ __forceinline__ A wave_max(A x)
     x = take_max(x, dpp_or_lowest<0x143, 0xc>(x));
     return at_lane(x, 63);
 }
+template <int CTRL, int ROWS> __device__ __forceinline__ float dpp_or_none(float x)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ double dpp_or_none(double x) { return dpp_or_zero<CTRL, ROWS>(x); }
+// the sum over the wave's 64 lanes, in a fixed order
+template <typename A> __device__ __forceinline__ A wave_sum(A x)
+{
+    x += dpp_or_none<0x111, 0xf>(x);
+    x += dpp_or_none<0x112, 0xf>(x);
+    x += dpp_or_none<0x114, 0xf>(x);
+    x += dpp_or_none<0x118, 0xf>(x);
+    x += dpp_or_none<0x142, 0xa>(x);
+    x += dpp_or_none<0x143, 0xc>(x);
+    return at_lane(x, 63);
+}
 template <typename A> __device__ __forceinline__ A sum_over(A x, int lanes)
 {
     for (int o = lanes / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, WAVE);
@@ -174,9 +211,68 @@ template <typename A> struct Stat {
     __device__ __forceinline__ void join_wave()
     {
         raise(wave_max(M));
-        s = sum_over(s, WAVE);
-        t = sum_over(t, WAVE);
+        s = wave_sum(s);
+        t = wave_sum(t);
     }
+};
+
+// What a lane gathers on its way over a long row; done() turns it into a Stat with M = the largest margin met.
+// fp64: the Stat itself.
+template <typename A> struct Gather {
+    Stat<A> q;
+    A mx;                               // the largest margin, -inf: none
+    __device__ __forceinline__ void init() { q.init(), mx = minus_inf(A()); }
+    template <int E> __device__ __forceinline__ void take(const A (&x)[E], A top)
+    {
+        mx = take_max(mx, top);
+        q.raise(take_max(q.M, top));
+#pragma unroll
+        for (int e = 0; e < E; ++e) q.add(x[e]);
+    }
+    __device__ __forceinline__ Stat<A> done() const { return q; }
+    __device__ __forceinline__ bool beyond() const { return false; }
+};
+// fp32: a margin costs a fused multiply-add, 2^x, an addition, a clamp and a fused multiply-add; the kernel is as much bound
+// by these as by memory.  s and t are kept relative to a power of two: s = sum 2^(c z - M2), t = sum 2^(c z - M2) (c z - M2)
+// with c = log2 e rounded and M2 = c R rounded, both exactly what the multiply-add uses, so that the rounding of M2 is known
+// (r = c R - M2) and taken out at the end.  R follows the largest margin only when it falls more than 13 behind: the terms
+// stay below e^13.  c z overflows for |z| > 2.3e38: rows whose largest margin lies out there are gathered by a Stat instead.
+template <> struct Gather<float> {
+    float R, M2, s, t, mx;
+    static __device__ __forceinline__ float edge() { return 2e38f; }
+    static __device__ __forceinline__ float c() { return 1.44269504f; }
+    __device__ __forceinline__ void init()
+    {
+        R = -edge(), M2 = -edge() * c();
+        s = t = 0.0f;
+        mx = minus_inf(0.0f);
+    }
+    template <int E> __device__ __forceinline__ void take(const float (&x)[E], float top)
+    {
+        mx = fmaxf(mx, top);
+        if (__ballot(top - R > 13.0f)) {
+            const float to = fmaxf(R, top), m2 = to * c(), d = fmaxf(M2 - m2, -1e4f), f = __builtin_amdgcn_exp2f(d);
+            t = (t + s * d) * f;
+            s *= f;
+            R = to, M2 = m2;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = fmaf(x[e], c(), -M2), ex = __builtin_amdgcn_exp2f(d);
+            s += ex;
+            t = fmaf(ex, fmaxf(d, -1e4f), t);
+        }
+    }
+    __device__ __forceinline__ Stat<float> done() const
+    {
+        const float r = fmaf(c(), R, -M2), f = __builtin_amdgcn_exp2f(-r);
+        Stat<float> q;
+        q.M = R, q.s = s * f, q.t = (t - r * s) * f * (1.0f / c());
+        if (s == 0.0f) q.init();
+        else if (mx > R) q.raise(mx);
+        return q;
+    }
+    __device__ __forceinline__ bool beyond() const { return !(fabsf(mx) < edge()) && mx != minus_inf(0.0f); }
 };
 
 // One row's answer.  s == 0: no class is left; s != s: the row holds NaN or +inf at an allowed class.
@@ -195,12 +291,12 @@ template <typename A> struct Answer {
 
 __device__ __forceinline__ bool allowed_bit(const uint32_t *mask, int64_t c) { return (mask[c >> 5] >> (c & 31)) & 1u; }
 
-// ---- top alternatives: lane i < k of the wave holds the i-th best (value, class) seen, -inf where there is none --------
+// ---- a sorted list of alternatives: lane i < k of the wave holds the i-th best (value, class) seen, -inf where there is none --------
 template <typename A> struct Best {
     A v;
     int id;
     A least;                            // the k-th best value: what does not exceed it is not taken
-    __device__ __forceinline__ void init() { v = least = minus_inf(A()), id = -1; }
+    __device__ __forceinline__ void init() { v = least = hidden_minus_inf(A()), id = -1; }
     // value m of class c goes behind the values >= m: classes come in ascending order, so a tie stays with the lower one
     __device__ __forceinline__ void insert(A m, int c, int lane, int k)
     {
@@ -236,27 +332,57 @@ template <typename A> struct Best {
             insert(m, cls, lane, k);
         } while (__ballot(lm > least));
     }
-    // the k best of `lists` sorted lists (value and class at [list * k + i]) whose classes ascend from list to list
-    __device__ __forceinline__ void merge(const A *vals, const int *ids, int lists, int lane, int k)
-    {
-        init();
-        int h = 0;
-        A head = lane < lists ? vals[lane * k] : minus_inf(A());
-        int hid = lane < lists ? ids[lane * k] : -1;
-        for (int i = 0; i < k; ++i) {
-            const A m = wave_max(head);
-            if (m == minus_inf(A())) break;
-            const int who = __ffsll((unsigned long long)__ballot(head == m)) - 1;
-            const int c = __builtin_amdgcn_readlane(hid, who);
-            if (lane == i) v = m, id = c;
-            if (lane == who) {
-                ++h;
-                head = h < k ? vals[lane * k + h] : minus_inf(A());
-                hid = h < k ? ids[lane * k + h] : -1;
-            }
+};
+
+// The k best of N candidates in LDS by counting, for each, the better ones (a tie: the lower class): slot[rank] = candidate.
+// Called by all `threads` of a workgroup between barriers; slots that no candidate takes keep what they hold.  Sixteen lanes
+// share a candidate, so that forty of them wait for LDS three times and not forty.
+template <typename A>
+__device__ __forceinline__ void rank_candidates(const A *val, const int *id, int N, int k, int threads, A *slot_v, int *slot_id)
+{
+    const int l = threadIdx.x & 15;
+    for (int i = threadIdx.x >> 4; i < N; i += threads >> 4) {
+        const A v = val[i];
+        const int c = id[i];
+        int rank = 0;
+        for (int j = l; j < N; j += 16) {
+            const A o = val[j];
+            rank += (int)(o > v) | ((int)(o == v) & (int)(id[j] < c));
+        }
+        rank += __builtin_amdgcn_update_dpp(0, rank, 0x128, 0xf, 0xf, false);          // rotations inside a row of 16 lanes
+        rank += __builtin_amdgcn_update_dpp(0, rank, 0x124, 0xf, 0xf, false);
+        rank += __builtin_amdgcn_update_dpp(0, rank, 0x122, 0xf, 0xf, false);
+        rank += __builtin_amdgcn_update_dpp(0, rank, 0x121, 0xf, 0xf, false);
+        if (l == 0 && rank < k) slot_v[rank] = v, slot_id[rank] = c;
+    }
+}
+
+// A value that at least c of the wave's 64 lanes reach (c >= 1), as large as it comes cheaply; -inf where fewer hold more than
+// that.  Up to 24: the c-th largest, one wave maximum after the other.  Beyond: the smallest of the maxima of 32 pairs, or of all.
+template <typename A> __device__ __forceinline__ A reached_by(A v, int c)
+{
+    if (c <= 24) {
+        A m;
+        for (;;) {
+            m = wave_max(v);
+            const unsigned long long b = __ballot(v == m);
+            c -= __popcll(b);
+            if (c <= 0 || m == minus_inf(A())) return m;
+            v = v == m ? minus_inf(A()) : v;
         }
     }
-};
+    if (c <= 32) v = take_max(v, __shfl_xor(v, 1, WAVE));
+    return -wave_max(-v);
+}
+// the q-th largest of `count` <= 64 values in LDS, by all lanes of a wave; -inf where fewer are more than that
+template <int COUNT, typename A> __device__ __forceinline__ A kth_of(const A *vals, int q, int lane)
+{
+    const A v = lane < COUNT ? vals[lane] : minus_inf(A());
+    int ge = 0;                                                        // how many reach this lane's value
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j) ge += vals[j] >= v ? 1 : 0;
+    return wave_max(ge >= q ? v : minus_inf(A()));
+}
 
 template <typename T> __device__ __forceinline__ typename Acc<T>::type margin_of(const LogprobsArgs &a, int64_t row, int64_t c)
 {
@@ -266,10 +392,10 @@ template <typename T> __device__ __forceinline__ typename Acc<T>::type margin_of
     return (A)((const T *)a.Z)[row * a.ldz + c];
 }
 
-// the outputs of one row by one wave: zy is the margin of given class `lane` (lanes < m)
+// the outputs of one row by one wave: zy is the margin of given class `lane` (lanes < m), alt that of alternative `lane`
 template <typename T, bool TOP>
 __device__ __forceinline__ void write_row(const LogprobsArgs &a, int64_t row, int lane, const Stat<typename Acc<T>::type> &q,
-                                          int y, typename Acc<T>::type zy, const Best<typename Acc<T>::type> &best)
+                                          int y, typename Acc<T>::type zy, typename Acc<T>::type alt, int alt_id)
 {
     typedef typename Acc<T>::type A;
     const Answer<A> w(q);
@@ -280,29 +406,84 @@ __device__ __forceinline__ void write_row(const LogprobsArgs &a, int64_t row, in
     }
     if (lane < a.m) ((A *)a.logp)[row * a.m + lane] = y < 0 ? A(0) : y >= a.C ? nan_of(A()) : w.logp(zy);
     if (TOP && lane < a.k) {
-        const bool none = !(q.s == q.s) || best.v == minus_inf(A());
-        a.top_ids[row * a.k + lane] = none ? -1 : best.id;
-        ((A *)a.top_logp)[row * a.k + lane] = w.logp(best.v);
+        a.top_ids[row * a.k + lane] = q.s == q.s ? alt_id : -1;
+        ((A *)a.top_logp)[row * a.k + lane] = w.logp(alt);
     }
 }
 
 // ---- rows of many classes: WAVES waves share a row, or one of `parts` stretches of it ---------------------------------
 // Each wave walks a stretch of its own, AHEAD loads of 16 bytes per lane in flight.
+//
+// Alternatives: every lane knows the largest margin it has met.  If c lanes of each of q waves hold at least tau and c q >= k,
+// no alternative is below tau: tau is the q-th largest over the waves of their c-th largest lane maximum, with c = ceil(k /
+// waves) and q = ceil(k / c).  Only lanes whose maximum reaches tau read their margins again and put those >= tau
+// into LDS (a little more than k on ordinary rows), where they are ranked.  More than CAND of them (rows full of ties, or
+// whose large margins sit in few lanes): the waves go over their stretches again, each keeping a sorted list.
+template <typename T> struct Stretch {
+    typedef typename Acc<T>::type A;
+    static constexpr int E = Vec<T>::E, STEP = WAVE * E;
+    const T *z;
+    const uint32_t *mask;
+    int64_t first, end;
+    // the 16 bytes of column c1 + lane E and the word with their bits, where the wave's step from c1 is `whole` inside the
+    // row, and where it reaches beyond the end; nothing here waits for what is loaded
+    __device__ __forceinline__ void load(int64_t c1, int lane, bool whole, Raw &raw, uint32_t &word) const
+    {
+        word = 0;
+        if (whole) {
+            raw = Vec<T>::load(z + c1 + lane * E);
+            if (mask) word = (mask + (c1 >> 5))[lane * E >> 5];
+            return;
+        }
+        load_any(c1 + lane * E, raw, word);
+    }
+    __device__ __forceinline__ void load_any(int64_t c, Raw &raw, uint32_t &word) const
+    {
+        raw = Raw{0, 0, 0, 0};
+        word = 0;
+        if (c + E <= end) {
+            raw = Vec<T>::load(z + c);
+        } else if (c < end) {                                          // the row's last, partial vector
+            T tail[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) tail[e] = z[c + e < end ? c + e : end - 1];
+            raw = __builtin_bit_cast(Raw, tail);
+        }
+        if (mask && c < end) word = mask[c >> 5];
+    }
+    // their margins, -inf where nothing takes part
+    __device__ __forceinline__ void get(int64_t c, const Raw &raw, uint32_t word, bool whole, A (&x)[E]) const
+    {
+        unpack(raw, x, T());
+        if (mask || !whole) {
+            uint32_t bits = mask ? word >> (c & 31) : (1u << E) - 1;
+            if (!whole) bits = c >= end ? 0 : c + E > end ? bits & ((1u << (int)(end - c)) - 1) : bits;
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = keep_if(x[e], (int)(bits << (31 - e)) >> 31);
+        }
+    }
+};
+
+constexpr int CAND = 1024;
+
 template <typename T, int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES *WAVE) void logprobs_wide_kernel(LogprobsArgs a)
 {
     typedef typename Acc<T>::type A;
-    constexpr int E = Vec<T>::E, STEP = WAVE * E, AHEAD = sizeof(T) == 8 ? 2 : 4;
-    __shared__ A sh_stat[WAVES][3];
-    __shared__ A sh_val[TOP && WAVES > 1 ? WAVES * WAVE : 1];
-    __shared__ int sh_id[TOP && WAVES > 1 ? WAVES * WAVE : 1];
-    const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE;
+    typedef Stretch<T> S;
+    constexpr int E = S::E, STEP = S::STEP, AHEAD = sizeof(T) == 8 ? 2 : 4;
+    static_assert(WAVES * WAVE <= CAND, "a sorted list of every wave fits");
+    __shared__ A sh_stat[WAVES][3], sh_kth[WAVES];
+    __shared__ A sh_val[TOP ? CAND : 1], sh_slot[TOP ? WAVE : 1];
+    __shared__ int sh_id[TOP ? CAND : 1], sh_slot_id[TOP ? WAVE : 1], sh_count;
+    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int part = blockIdx.x;
     for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
-        const T *z = (const T *)a.Z + row * a.ldz;
-        const uint32_t *mask = a.allowed ? a.allowed + row * a.ld_allowed : nullptr;
-        const int64_t first = ((int64_t)part * WAVES + wave) * a.per_wave;
-        const int64_t end = first + a.per_wave < a.width ? first + a.per_wave : a.width;
+        S in;
+        in.z = (const T *)a.Z + row * a.ldz;
+        in.mask = a.allowed ? a.allowed + row * a.ld_allowed : nullptr;
+        in.first = ((int64_t)part * WAVES + wave) * a.per_wave;
+        in.end = in.first + a.per_wave < a.width ? in.first + a.per_wave : a.width;
         // given classes: their margins are on the way while the row is read
         int y = -1;
         A zy = A(0);
@@ -310,96 +491,170 @@ __global__ __launch_bounds__(WAVES *WAVE) void logprobs_wide_kernel(LogprobsArgs
             y = a.labels[row * a.m + lane];
             if (y >= 0 && y < a.C) zy = margin_of<T>(a, row, y);
         }
-        Stat<A> q;
-        q.init();
-        Best<A> best;
-        best.init();
-        for (int64_t c0 = first; c0 < end; c0 += AHEAD * STEP) {
+        Gather<A> acc;
+        acc.init();
+        // the lane's second and third largest maximum of a vector (acc.mx is the largest), and the steps of the first two
+        A v2 = minus_inf(A()), v3 = minus_inf(A());
+        int at1 = 0, at2 = 0;
+        for (int64_t c1 = in.first; c1 < in.end; c1 += AHEAD * STEP) {
             Raw raw[AHEAD];
-            uint32_t bits[AHEAD];
+            uint32_t word[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) in.load(c1 + u * STEP, lane, c1 + (u + 1) * STEP <= in.end, raw[u], word[u]);
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const int64_t c = c0 + u * STEP + lane * E;
-                raw[u] = Raw{0, 0, 0, 0};
-                bits[u] = 0;
-                if (c + E <= end) {
-                    raw[u] = Vec<T>::load(z + c);
-                    bits[u] = (1u << E) - 1;
-                } else if (c < end) {                                  // the row's last, partial vector
-                    T tail[E];
-#pragma unroll
-                    for (int e = 0; e < E; ++e) tail[e] = z[c + e < end ? c + e : end - 1];
-                    raw[u] = __builtin_bit_cast(Raw, tail);
-                    bits[u] = (1u << (int)(end - c)) - 1;
-                }
-                if (mask && c < end) bits[u] &= mask[c >> 5] >> (c & 31);
-            }
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (c0 + u * STEP >= end) break;
+                if (c1 + u * STEP >= in.end) break;
                 A x[E];
-                unpack(raw[u], x, T());
-                if (mask || c0 + (u + 1) * STEP > end) {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = (bits[u] >> e) & 1u ? x[e] : minus_inf(A());
-                }
+                in.get(c1 + u * STEP + lane * E, raw[u], word[u], c1 + (u + 1) * STEP <= in.end, x);
                 A top = x[0];
 #pragma unroll
                 for (int e = 1; e < E; ++e) top = take_max(top, x[e]);
-                q.raise(take_max(q.M, top));
-#pragma unroll
-                for (int e = 0; e < E; ++e) q.add(x[e]);
-                if (TOP) best.take(x, (int)(c0 + u * STEP + lane * E), lane, a.k);
+                if (TOP) {
+                    const bool over1 = top > acc.mx, over2 = top > v2;
+                    const int here = (int)(c1 + u * STEP - in.first);
+                    v3 = over2 ? v2 : take_max(v3, top);
+                    at2 = over1 ? at1 : over2 ? here : at2;
+                    v2 = over1 ? acc.mx : over2 ? top : v2;
+                    at1 = over1 ? here : at1;
+                }
+                acc.take(x, top);
             }
         }
-        // the reference class, behind all others
-        if (a.reference && part == a.parts - 1 && wave == WAVES - 1 && (!mask || allowed_bit(mask, a.width))) {
-            if (lane == 0) {
-                q.raise(take_max(q.M, A(0)));
-                q.add(A(0));
+        const A v1 = acc.mx;
+        Stat<A> q = acc.done();
+        if (sizeof(T) == 4 || std::is_same<T, __bf16>::value) {
+            if (__ballot(acc.beyond())) {
+                q.init();
+                for (int64_t c1 = in.first; c1 < in.end; c1 += STEP) {
+                    Raw raw;
+                    uint32_t word;
+                    A x[E];
+                    in.load_any(c1 + lane * E, raw, word);
+                    in.get(c1 + lane * E, raw, word, false, x);
+                    for (int e = 0; e < E; ++e) {
+                        q.raise(take_max(q.M, x[e]));
+                        q.add(x[e]);
+                    }
+                }
             }
-            if (TOP && A(0) > best.least) best.insert(A(0), (int)a.width, lane, a.k);
+        }
+        // the reference class, behind all others, is lane 0's of the last wave
+        const bool with_ref = a.reference && part == a.parts - 1 && wave == WAVES - 1 && lane == 0 &&
+                              (!in.mask || allowed_bit(in.mask, a.width));
+        if (with_ref) {
+            q.raise(take_max(q.M, A(0)));
+            q.add(A(0));
+        }
+        const int c = (a.k + WAVES - 1) / WAVES;
+        A kth = minus_inf(A());
+        if (TOP) {
+            kth = reached_by(with_ref ? take_max(v1, A(0)) : v1, c);
+            if (threadIdx.x == 0) sh_count = 0;
+            if (threadIdx.x < WAVE) sh_slot[lane] = minus_inf(A()), sh_slot_id[lane] = -1;
         }
         q.join_wave();
-        if (WAVES > 1) {
-            if (lane == 0) sh_stat[wave][0] = q.M, sh_stat[wave][1] = q.s, sh_stat[wave][2] = q.t;
-            if (TOP && lane < a.k) sh_val[wave * a.k + lane] = best.v, sh_id[wave * a.k + lane] = best.id;
+        if (lane == 0) sh_stat[wave][0] = q.M, sh_stat[wave][1] = q.s, sh_stat[wave][2] = q.t, sh_kth[wave] = kth;
+        __syncthreads();
+        if (TOP) {
+            A tau = kth;
+            if (WAVES > 1) tau = kth_of<WAVES>(sh_kth, (a.k + c - 1) / c, lane);
+            tau = take_max(tau, lowest(A()));                          // -inf is no alternative
+            auto put = [&](int64_t col, const A (&x)[E]) {
+                uint32_t hit = 0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) hit |= (uint32_t)(x[e] >= tau) << e;
+                if (!hit) return;
+                int at = atomicAdd(&sh_count, __popc(hit));
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if ((hit >> e) & 1u) {
+                        if (at < CAND) sh_val[at] = x[e], sh_id[at] = (int)(col + e);
+                        ++at;
+                    }
+            };
+            if (v1 >= tau) {
+                Raw raw, more;
+                uint32_t word, bits;
+                A x[E];
+                if (v3 < tau) {                                        // all of the lane's are in one vector or two
+                    const int64_t col = in.first + lane * E;
+                    in.load_any(col + at1, raw, word);
+                    if (v2 >= tau) in.load_any(col + at2, more, bits);
+                    in.get(col + at1, raw, word, false, x);
+                    put(col + at1, x);
+                    if (v2 >= tau) {
+                        in.get(col + at2, more, bits, false, x);
+                        put(col + at2, x);
+                    }
+                } else {
+                    for (int64_t col = in.first + lane * E; col < in.end; col += STEP) {
+                        in.load_any(col, raw, word);
+                        in.get(col, raw, word, false, x);
+                        put(col, x);
+                    }
+                }
+            }
+            if (with_ref && A(0) >= tau) {
+                const int at = atomicAdd(&sh_count, 1);
+                if (at < CAND) sh_val[at] = A(0), sh_id[at] = (int)a.width;
+            }
             __syncthreads();
-            if (wave == 0) {
+            int N = sh_count;
+            if (N > CAND) {
+                __syncthreads();
+                Best<A> best;
+                best.init();
+                for (int64_t c1 = in.first; c1 < in.end; c1 += STEP) {
+                    Raw raw;
+                    uint32_t word;
+                    A x[E];
+                    in.load_any(c1 + lane * E, raw, word);
+                    in.get(c1 + lane * E, raw, word, false, x);
+                    best.take(x, (int)(c1 + lane * E), lane, a.k);
+                }
+                if (__ballot(with_ref) && A(0) > best.least) best.insert(A(0), (int)a.width, lane, a.k);
+                if (lane < a.k) sh_val[wave * a.k + lane] = best.v, sh_id[wave * a.k + lane] = best.id;
+                N = WAVES * a.k;
+                __syncthreads();
+            }
+            rank_candidates(sh_val, sh_id, N, a.k, WAVES * WAVE, sh_slot, sh_slot_id);
+            __syncthreads();
+        }
+        if (wave == 0) {
+            if (WAVES > 1) {
                 q.init();
                 if (lane < WAVES) q.M = sh_stat[lane][0], q.s = sh_stat[lane][1], q.t = sh_stat[lane][2];
                 q.join_wave();
-                if (TOP) best.merge(sh_val, sh_id, WAVES, lane, a.k);
             }
-        }
-        if (wave == 0) {
+            const A tv = TOP ? sh_slot[lane] : A(0);
+            const int ti = TOP ? sh_slot_id[lane] : -1;
             if (a.parts == 1) {
-                write_row<T, TOP>(a, row, lane, q, y, zy, best);
+                write_row<T, TOP>(a, row, lane, q, y, zy, tv, ti);
             } else {
                 const int64_t item = row * a.parts + part;
                 if (lane == 0) {
                     A *w = (A *)a.ws_stat + item * 3;
                     w[0] = q.M, w[1] = q.s, w[2] = q.t;
                 }
-                if (TOP && lane < a.k) ((A *)a.ws_val)[item * a.k + lane] = best.v, a.ws_id[item * a.k + lane] = best.id;
+                if (TOP && lane < a.k) ((A *)a.ws_val)[item * a.k + lane] = tv, a.ws_id[item * a.k + lane] = ti;
             }
         }
-        if (WAVES > 1) __syncthreads();
+        __syncthreads();
     }
 }
 
-// the parts of a row joined, a wave per row
-template <typename T, bool TOP> __global__ __launch_bounds__(WAVE) void logprobs_join_kernel(LogprobsArgs a)
+// The parts of a row joined, a workgroup per row.  No alternative of the row is below the k-th of any part.
+template <typename T, bool TOP> __global__ __launch_bounds__(TOP ? VEC_BLOCK : WAVE) void logprobs_join_kernel(LogprobsArgs a)
 {
     typedef typename Acc<T>::type A;
-    __shared__ A sh_val[TOP ? LOGPROBS_MAX_PARTS * WAVE : 1];
-    __shared__ int sh_id[TOP ? LOGPROBS_MAX_PARTS * WAVE : 1];
-    const int lane = threadIdx.x;
+    __shared__ A sh_val[TOP ? LOGPROBS_MAX_PARTS * WAVE : 1], sh_slot[TOP ? WAVE : 1];
+    __shared__ int sh_id[TOP ? LOGPROBS_MAX_PARTS * WAVE : 1], sh_slot_id[TOP ? WAVE : 1], sh_count;
+    const int lane = threadIdx.x & (WAVE - 1);
     for (int64_t row = blockIdx.x; row < a.n; row += gridDim.x) {
         int y = -1;
         A zy = A(0);
-        if (lane < a.m) {
-            y = a.labels[row * a.m + lane];
+        if (threadIdx.x < a.m) {
+            y = a.labels[row * a.m + threadIdx.x];
             if (y >= 0 && y < a.C) zy = margin_of<T>(a, row, y);
         }
         Stat<A> q;
@@ -408,16 +663,25 @@ template <typename T, bool TOP> __global__ __launch_bounds__(WAVE) void logprobs
             const A *w = (const A *)a.ws_stat + (row * a.parts + lane) * 3;
             q.M = w[0], q.s = w[1], q.t = w[2];
         }
-        Best<A> best;
-        best.init();
         if (TOP) {
             const int64_t at = row * a.parts * a.k;
-            for (int i = lane; i < a.parts * a.k; i += WAVE) sh_val[i] = ((const A *)a.ws_val)[at + i], sh_id[i] = a.ws_id[at + i];
+            const A tau = wave_max(lane < a.parts ? ((const A *)a.ws_val)[at + lane * a.k + a.k - 1] : minus_inf(A()));
+            if (threadIdx.x == 0) sh_count = 0;
+            if (threadIdx.x < WAVE) sh_slot[lane] = minus_inf(A()), sh_slot_id[lane] = -1;
+            __syncthreads();
+            for (int i = threadIdx.x; i < a.parts * a.k; i += VEC_BLOCK) {
+                const A v = ((const A *)a.ws_val)[at + i];
+                if (v >= tau && v > minus_inf(A())) {
+                    const int slot = atomicAdd(&sh_count, 1);
+                    sh_val[slot] = v, sh_id[slot] = a.ws_id[at + i];
+                }
+            }
+            __syncthreads();
+            rank_candidates(sh_val, sh_id, sh_count, a.k, VEC_BLOCK, sh_slot, sh_slot_id);
             __syncthreads();
         }
         q.join_wave();
-        if (TOP) best.merge(sh_val, sh_id, a.parts, lane, a.k);
-        write_row<T, TOP>(a, row, lane, q, y, zy, best);
+        if (threadIdx.x < WAVE) write_row<T, TOP>(a, row, lane, q, y, zy, TOP ? sh_slot[lane] : A(0), TOP ? sh_slot_id[lane] : -1);
         if (TOP) __syncthreads();
     }
 }
@@ -521,12 +785,12 @@ template <typename T> __global__ __launch_bounds__(VEC_BLOCK) void logprobs_grad
         T *dz = (T *)a.dZ + row * a.lddz;
         const uint32_t *mask = a.allowed ? a.allowed + row * a.ld_allowed : nullptr;
         Raw raw[U];
-        uint32_t bits[U];
+        uint32_t word[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t c = c0 + (u * VEC_BLOCK + threadIdx.x) * E;
             raw[u] = Raw{0, 0, 0, 0};
-            bits[u] = (1u << E) - 1;
+            word[u] = 0xffffffffu;
             if (c + E <= a.width) {
                 raw[u] = Vec<T>::load(z + c);
             } else if (c < a.width) {
@@ -535,7 +799,7 @@ template <typename T> __global__ __launch_bounds__(VEC_BLOCK) void logprobs_grad
                 for (int e = 0; e < E; ++e) tail[e] = z[c + e < a.width ? c + e : a.width - 1];
                 raw[u] = __builtin_bit_cast(Raw, tail);
             }
-            if (mask && c < a.width) bits[u] = mask[c >> 5] >> (c & 31);
+            if (mask && c < a.width) word[u] = mask[c >> 5];
         }
         int y = -1;
         A gy = A(0);
@@ -545,7 +809,7 @@ template <typename T> __global__ __launch_bounds__(VEC_BLOCK) void logprobs_grad
         }
         RowGrad<A> w;
         w.load(a, row);
-        w.G += sum_over(gy, WAVE);
+        w.G += wave_sum(gy);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t cw = c0 + (u * VEC_BLOCK + (threadIdx.x - lane)) * E;     // the wave's stretch
@@ -554,7 +818,7 @@ template <typename T> __global__ __launch_bounds__(VEC_BLOCK) void logprobs_grad
             A x[E];
             unpack(raw[u], x, T());
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = w.empty || !((bits[u] >> e) & 1u) ? A(0) : w.at(x[e]);
+            for (int e = 0; e < E; ++e) x[e] = w.empty || !((word[u] >> ((c & 31) + e)) & 1u) ? A(0) : w.at(x[e]);
             for (unsigned long long b = __ballot(gy != A(0) && y >= cw && y < cw + WAVE * E); b; b &= b - 1) {
                 const int from = __ffsll(b) - 1;
                 const int64_t yy = __builtin_amdgcn_readlane(y, from);
@@ -634,17 +898,26 @@ void logprobs_plan(int dtype, int64_t n, int64_t C, int64_t width, int k, int nu
     a->per_wave = 0;
     if (C <= WAVE * NARROW_PER_LANE) return;
     const int64_t steps = (width + step - 1) / step;                   // loads of a whole wave that the row takes
-    a->waves = steps <= 8 ? 1 : 4;
-    if (n < 2 * num_cus && steps > 16) {
-        a->waves = 16;
-        int64_t parts = (steps + 16 * 8 - 1) / (16 * 8);
-        if (n < num_cus) {
-            const int64_t fill = (num_cus + n - 1) / n;
-            if (parts < fill) parts = fill;
+    const int most = dtype == SSN_F64 ? 8 : 16, ahead = dtype == SSN_F64 ? 2 : 4;
+    // Rows enough to fill the chip: as few waves per row as keep its loads in flight, since joining them costs (3000 rows of
+    // 5000 fp32: one wave 21 us, four 24 us, eight 35 us; 8192 of 65536 bf16: four 187 us, eight 179 us, sixteen 238 us).
+    // Fewer rows than compute units: all the waves a workgroup may have, and several workgroups per row where each wave
+    // still has loads for one round of AHEAD (one row of 131072 fp32: one workgroup 18 us, eight 11 us; of 32000: one 9.2 us,
+    // two 10.3 us, since the join is a launch of its own).
+    if (steps <= 8 || (steps <= 24 && n >= 8 * num_cus)) {
+        a->waves = 1;
+    } else if (n >= 2 * num_cus) {
+        a->waves = steps <= 64 ? 4 : 8;
+    } else if (n >= num_cus) {
+        a->waves = 8;
+    } else {
+        a->waves = most;
+        if (steps > 2 * most * ahead) {
+            int64_t parts = (steps + most * ahead - 1) / (most * ahead);
+            if (parts > num_cus / n) parts = num_cus / n;
+            if (parts > LOGPROBS_MAX_PARTS) parts = LOGPROBS_MAX_PARTS;
+            a->parts = (int)parts;
         }
-        if (parts > (steps + 31) / 32) parts = (steps + 31) / 32;
-        if (parts > LOGPROBS_MAX_PARTS) parts = LOGPROBS_MAX_PARTS;
-        a->parts = (int)parts;
     }
     const int64_t shares = (int64_t)a->parts * a->waves;
     a->per_wave = (steps + shares - 1) / shares * step;
@@ -685,10 +958,11 @@ hipError_t launch_logprobs(int dtype, LogprobsArgs &a, void *workspace, hipStrea
         };
         if (a.waves == 1) wide(std::integral_constant<int, 1>());
         else if (a.waves == 4) wide(std::integral_constant<int, 4>());
-        else wide(std::integral_constant<int, 16>());
+        else if (a.waves == 8) wide(std::integral_constant<int, 8>());
+        else if constexpr (sizeof(T) < 8) wide(std::integral_constant<int, 16>());
         if (a.parts > 1) {
             const dim3 rows((unsigned)(a.n < MAX_GRID ? a.n : MAX_GRID));
-            if (a.k) hipLaunchKernelGGL((logprobs_join_kernel<T, true>), rows, dim3(WAVE), 0, st, a);
+            if (a.k) hipLaunchKernelGGL((logprobs_join_kernel<T, true>), rows, dim3(VEC_BLOCK), 0, st, a);
             else hipLaunchKernelGGL((logprobs_join_kernel<T, false>), rows, dim3(WAVE), 0, st, a);
         }
     });

@@ -2203,8 +2203,8 @@ int ssn_logprobs(const ssn_rows *r, void *logp, void *maxpart, void *logpart, vo
     SSN_TRY(current_cus(&cus));
     logprobs_plan(r->dtype, a.n, a.C, a.width, a.k, cus, &a);
     const int64_t need = logprobs_workspace(r->dtype, a.n, a.k, a);
-    if (need > 0 && (!workspace || !aligned_to(workspace, 8))) return SSN_E_INVALID_ARG;
     if (need > workspace_bytes) return SSN_E_TOO_LARGE;
+    if (need > 0 && (!workspace || !aligned_to(workspace, 8))) return SSN_E_INVALID_ARG;
     return launch_logprobs(r->dtype, a, workspace, (hipStream_t)r->stream) == hipSuccess ? SSN_OK : SSN_E_HIP;
 }
 
@@ -2269,8 +2269,8 @@ int ssn_q4_margins(const ssn_q4 *b, int32_t dtype, int64_t n, const void *X, int
     a.zdtype = zdtype;
     SSN_TRY(q4_parts(&a));
     const int64_t need = q4_workspace(a);
-    if (need > 0 && (!workspace || !aligned_to(workspace, 4))) return SSN_E_INVALID_ARG;
     if (need > workspace_bytes) return SSN_E_TOO_LARGE;
+    if (need > 0 && (!workspace || !aligned_to(workspace, 4))) return SSN_E_INVALID_ARG;
     return launch_q4_margins(a, workspace, (hipStream_t)stream) == hipSuccess ? SSN_OK : SSN_E_HIP;
 }
 
