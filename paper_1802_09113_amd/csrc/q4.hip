@@ -43,6 +43,7 @@ template <> struct Rows<__bf16> {
         const B2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3);
         return Op{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
+    static __device__ __forceinline__ void operand(const Raw (&r)[1], Op (&o)[1]) { o[0] = __builtin_bit_cast(Op, r[0]); }
     static __device__ __forceinline__ void load(const __bf16 *x, Op (&o)[1]) { o[0] = __builtin_bit_cast(Op, (Raw) * (const RawAt2 *)x); }
     static __device__ __forceinline__ F4 mul(Op x, Op w, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, c, 0, 0, 0); }
 };
@@ -55,6 +56,7 @@ template <> struct Rows<_Float16> {
         const H2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, 3);
         return Op{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
+    static __device__ __forceinline__ void operand(const Raw (&r)[1], Op (&o)[1]) { o[0] = __builtin_bit_cast(Op, r[0]); }
     static __device__ __forceinline__ void load(const _Float16 *x, Op (&o)[1]) { o[0] = __builtin_bit_cast(Op, (Raw) * (const RawAt2 *)x); }
     static __device__ __forceinline__ F4 mul(Op x, Op w, F4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, c, 0, 0, 0); }
 };
@@ -62,25 +64,36 @@ template <> struct Rows<float> {
     static constexpr int PIECES = 3;
     typedef B8 Op;
     static __device__ __forceinline__ Op codes(uint32_t w) { return Rows<__bf16>::codes(w); }
+    // the three parts of two features, a word of two bfloat16 numbers each
+    static __device__ __forceinline__ void split(const uint32_t (&u)[2], uint32_t (&word)[3])
+    {
+        uint32_t top[2][3];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float v = __uint_as_float(u[i]), v0 = __uint_as_float(u[i] & 0xffff0000u);
+            // cut, not rounded: x0 never overflows, and what is left has eight significant bits fewer.  +-inf - (+-inf) is no
+            // part of the value: 0 there
+            const float v1 = __builtin_isinf(v) ? 0.0f : v - v0;
+            const float w1 = __uint_as_float(__float_as_uint(v1) & 0xffff0000u);
+            top[i][0] = u[i], top[i][1] = __float_as_uint(v1), top[i][2] = __float_as_uint(v1 - w1);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) word[k] = (top[0][k] >> 16) | (top[1][k] & 0xffff0000u);
+    }
     static __device__ __forceinline__ void load(const float *x, Op (&o)[3])
     {
         const Raw r[2] = {*(const RawAt4 *)x, *(const RawAt4 *)(x + 4)};
+        operand(r, o);
+    }
+    static __device__ __forceinline__ void operand(const Raw (&r)[2], Op (&o)[3])
+    {
         uint32_t part[3][4];
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-            uint32_t top[2][3];
+            uint32_t word[3];
+            split({r[e / 4][e % 4], r[e / 4][e % 4 + 1]}, word);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t u = r[(e + i) / 4][(e + i) % 4];
-                const float v = __uint_as_float(u), v0 = __uint_as_float(u & 0xffff0000u);
-                // cut, not rounded: x0 never overflows, and what is left has eight significant bits fewer.  +-inf - (+-inf)
-                // is no part of the value: 0 there
-                const float v1 = __builtin_isinf(v) ? 0.0f : v - v0;
-                const float w1 = __uint_as_float(__float_as_uint(v1) & 0xffff0000u);
-                top[i][0] = u, top[i][1] = __float_as_uint(v1), top[i][2] = __float_as_uint(v1 - w1);
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k) part[k][e / 2] = (top[0][k] >> 16) | (top[1][k] & 0xffff0000u);
+            for (int k = 0; k < 3; ++k) part[k][e / 2] = word[k];
         }
 #pragma unroll
         for (int k = 0; k < 3; ++k) o[k] = __builtin_bit_cast(Op, Raw{part[k][0], part[k][1], part[k][2], part[k][3]});
@@ -111,99 +124,365 @@ __device__ __forceinline__ void store_margin(void *Z, int zdtype, int64_t at, fl
     else ((__bf16 *)Z)[at] = (__bf16)v;
 }
 
-// Four waves share a stretch of the blocks of OT tiles and add their sums in a fixed order.  Row r of a group of 16 stands
+// eight consecutive margins of a row, of which `left` are inside it
+template <typename Z> __device__ __forceinline__ void store_margins(Z *z, int64_t left, const float (&v)[8])
+{
+    if (left >= 8) {
+        Z out[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = (Z)v[e];
+        Raw r[sizeof(Z) / 2];
+        __builtin_memcpy(r, out, sizeof(out));
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(Z) / 2; ++h) ((RawAt2 *)z)[h] = r[h];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < left) z[e] = (Z)v[e];
+    }
+}
+
+// `waves` waves share a stretch of the blocks of OT tiles and add their sums in a fixed order.  Row r of a group of 16 stands
 // at place 4 (r % 4) + r / 4 of the matrix operand: its sums are then in register r / 4 of lane group r % 4, and up to
-// four rows need one register of the four (USED = 1).
-constexpr int Q4_WAVES = 4;
-template <typename T, int GROUP, int RT, int USED, int OT>
-__global__ __launch_bounds__(Q4_WAVES *WAVE) void q4_stream_kernel(Q4Args a)
+// four rows need one register of the four (USED = 1).  Places without a row hold the last row again; their sums are not
+// stored.
+template <int GROUPS> struct ScaleWord;
+template <> struct ScaleWord<1> { typedef uint16_t type; };
+template <> struct ScaleWord<2> { typedef uint32_t type; };
+template <> struct ScaleWord<4> { typedef uint64_t type; };
+
+template <typename T, int GROUP, int USED, int OT, int WAVES, int DEPTH>
+__global__ __launch_bounds__(WAVES *WAVE) void q4_stream_kernel(Q4Args a)
 {
     typedef typename Rows<T>::Op Op;
     constexpr int PIECES = Rows<T>::PIECES, PER = GROUP / 32, GROUPS = BLOCK / GROUP;
-    __shared__ float sums[Q4_WAVES][RT * 4 * USED][OT * TILE];
-    const int lane = threadIdx.x & (WAVE - 1), wave = threadIdx.x / WAVE, o = lane & 15, g = lane >> 4;
-    const int64_t blocks = (a.p + BLOCK - 1) / BLOCK, tiles = (a.K + TILE - 1) / TILE;
-    const int64_t t0 = (int64_t)blockIdx.x * OT, r0 = (int64_t)blockIdx.z * (16 * RT);
-    const int64_t shares = (int64_t)a.parts * Q4_WAVES, mine = (int64_t)blockIdx.y * Q4_WAVES + wave;
+    typedef typename ScaleWord<GROUPS>::type Scales;
+    __shared__ float sums[WAVES][4 * USED][OT * TILE];
+    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), o = lane & 15, g = lane >> 4;
+    const int64_t blocks = (a.p + BLOCK - 1) / BLOCK, tiles = (a.K + TILE - 1) / TILE, whole = a.p / BLOCK;
+    const int64_t t0 = (int64_t)blockIdx.x * OT, r0 = (int64_t)blockIdx.z * 16;
+    const int64_t shares = (int64_t)a.parts * WAVES, mine = (int64_t)blockIdx.y * WAVES + wave;
     const int64_t first = blocks * mine / shares, last = blocks * (mine + 1) / shares;
 
-    const T *x[RT];
-    bool live[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int64_t r = r0 + rt * 16 + (o & 3) * 4 + (o >> 2);
-        live[rt] = r < a.n;
-        x[rt] = (const T *)a.X + (live[rt] ? r : 0) * a.ldx + 8 * g;
-    }
-    const uint8_t *w[OT];
-    const uint16_t *sc[OT];
+    const int64_t own = r0 + (o & 3) * 4 + (o >> 2);                   // the row at this lane's place
+    const T *x = (const T *)a.X + (own < a.n ? own : a.n - 1) * a.ldx + 8 * g;
+    const Raw *w[OT];
+    const Scales *sc[OT];
 #pragma unroll
     for (int ot = 0; ot < OT; ++ot) {
         const int64_t t = t0 + ot < tiles ? t0 + ot : tiles - 1;       // a tile twice at the end; its second sums are not stored
-        w[ot] = a.packed + t * blocks * (WAVE * 16) + lane * 16;
-        sc[ot] = a.scales + t * blocks * (TILE * GROUPS) + o * GROUPS;
+        w[ot] = (const Raw *)a.packed + t * blocks * WAVE;
+        sc[ot] = (const Scales *)a.scales + t * blocks * TILE;
     }
-    float acc[OT][RT][USED];
+    float acc[OT][USED];
 #pragma unroll
     for (int ot = 0; ot < OT; ++ot)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < USED; ++i) acc[ot][rt][i] = 0.0f;
+        for (int i = 0; i < USED; ++i) acc[ot][i] = 0.0f;
 
-#pragma unroll 2
-    for (int64_t b = first; b < last; ++b) {
-        Raw q[OT];
-        uint16_t s[OT][GROUPS];
-#pragma unroll
-        for (int ot = 0; ot < OT; ++ot) {
-            q[ot] = *(const Raw *)(w[ot] + b * (WAVE * 16));
-#pragma unroll
-            for (int i = 0; i < GROUPS; ++i) s[ot][i] = sc[ot][b * (TILE * GROUPS) + i];
-        }
-        F4 d[OT][RT];
+    // one block: xo(j) fills the rows' operands of word j
+    auto block = [&](const Raw (&q)[OT], const Scales (&s)[OT], auto rows) {
+        F4 d[OT];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            Op xo[RT][PIECES];
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-                for (int k = 0; k < PIECES; ++k) xo[rt][k] = __builtin_bit_cast(Op, Raw{0, 0, 0, 0});
-                if (live[rt]) row_operand<T>(x[rt], b * BLOCK + 32 * j, a.p - 8 * g, xo[rt]);
-            }
+            Op xo[PIECES];
+            rows(j, xo);
 #pragma unroll
             for (int ot = 0; ot < OT; ++ot) {
                 const Op wo = Rows<T>::codes(q[ot][j]);
+                const float f = bf16_value((uint16_t)(s[ot] >> (16 * (j / PER))));
+                if (j % PER == 0) d[ot] = F4{0, 0, 0, 0};
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    if (j % PER == 0) d[ot][rt] = F4{0, 0, 0, 0};
+                for (int k = PIECES - 1; k >= 0; --k) d[ot] = Rows<T>::mul(xo[k], wo, d[ot]);
+                if (j % PER == PER - 1) {
 #pragma unroll
-                    for (int k = PIECES - 1; k >= 0; --k) d[ot][rt] = Rows<T>::mul(xo[rt][k], wo, d[ot][rt]);
-                    if (j % PER == PER - 1) {
-                        const float f = bf16_value(s[ot][j / PER]);
-#pragma unroll
-                        for (int i = 0; i < USED; ++i) acc[ot][rt][i] = fmaf(f, d[ot][rt][i], acc[ot][rt][i]);
-                    }
+                    for (int i = 0; i < USED; ++i) acc[ot][i] = fmaf(f, d[ot][i], acc[ot][i]);
                 }
             }
         }
+    };
+    // fp32 rows, sixteen at most: a lane splits its share of each row once and the wave reads the operands from LDS; to split
+    // them where they are used would cost a lane four rows' work for one row
+    constexpr bool STAGED = PIECES == 3;
+    constexpr int ROWS = 4 * USED, LINE = BLOCK * 2 + 16;              // a row's 128 numbers, 16 bytes apart in the banks
+    __shared__ __align__(16) unsigned char stage[STAGED ? WAVES * 3 * ROWS * LINE : 16];
+    unsigned char *st = stage + (STAGED ? wave * 3 * ROWS * LINE : 0);
+    const int64_t stop = last < whole ? last : whole;
+    for (int64_t b = first; b < stop; b += DEPTH) {
+        Raw q[DEPTH][OT];
+        Scales s[DEPTH][OT];
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) {
+            const int64_t bb = b + u < stop ? b + u : stop - 1;        // fetched again where there is no such block
+#pragma unroll
+            for (int ot = 0; ot < OT; ++ot) {
+                q[u][ot] = (w[ot] + bb * WAVE)[lane];
+                s[u][ot] = (sc[ot] + bb * TILE)[o];
+            }
+        }
+        if constexpr (STAGED) {
+            typedef uint32_t Pair __attribute__((ext_vector_type(2), aligned(4)));
+            Pair v[DEPTH][ROWS];
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u)
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const int64_t bb = b + u < stop ? b + u : stop - 1;
+                    if (r0 + r < a.n) v[u][r] = *(const Pair *)((const float *)a.X + (r0 + r) * a.ldx + bb * BLOCK + 2 * lane);
+                }
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u) {
+                if (b + u >= stop) break;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+                    if (r0 + r < a.n) {
+                        uint32_t word[3];
+                        Rows<float>::split({v[u][r][0], v[u][r][1]}, word);
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) *(uint32_t *)(st + (k * ROWS + r) * LINE + 4 * lane) = word[k];
+                    }
+                // the wave's own LDS, which it reads and writes in order
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                const int row = own < a.n && own - r0 < ROWS ? (int)(own - r0) : 0;
+                block(q[u], s[u], [&](int j, Op (&xo)[PIECES]) {
+#pragma unroll
+                    for (int k = 0; k < PIECES; ++k)
+                        xo[k] = __builtin_bit_cast(Op, *(const Raw *)(st + (k * ROWS + row) * LINE + 64 * j + 16 * g));
+                });
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+            continue;
+        }
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) {
+            if (b + u >= stop) break;
+            block(q[u], s[u], [&](int j, Op (&xo)[PIECES]) {
+                Rows<T>::load(x + (b + u) * BLOCK + 32 * j, xo);
+            });
+        }
+    }
+    if (last > whole && first < last) {                                // features end inside the last block
+        Raw q[OT];
+        Scales s[OT];
+#pragma unroll
+        for (int ot = 0; ot < OT; ++ot) {
+            q[ot] = (w[ot] + whole * WAVE)[lane];
+            s[ot] = (sc[ot] + whole * TILE)[o];
+        }
+        block(q, s, [&](int j, Op (&xo)[PIECES]) {
+            row_operand<T>(x, whole * BLOCK + 32 * j, a.p - 8 * g, xo);
+        });
     }
 #pragma unroll
     for (int ot = 0; ot < OT; ++ot)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-            for (int i = 0; i < USED; ++i) sums[wave][rt * 4 * USED + i * 4 + g][ot * TILE + o] = acc[ot][rt][i];
+        for (int i = 0; i < USED; ++i) sums[wave][i * 4 + g][ot * TILE + o] = acc[ot][i];
     __syncthreads();
-    for (int e = threadIdx.x; e < RT * 4 * USED * OT * TILE; e += Q4_WAVES * WAVE) {
+    for (int e = threadIdx.x; e < 4 * USED * OT * TILE; e += WAVES * WAVE) {
         const int rr = e / (OT * TILE), cc = e % (OT * TILE);
         const int64_t r = r0 + rr, c = t0 * TILE + cc;
         if (r >= a.n || c >= a.K) continue;
         float v = sums[0][rr][cc];
 #pragma unroll
-        for (int i = 1; i < Q4_WAVES; ++i) v += sums[i][rr][cc];
+        for (int i = 1; i < WAVES; ++i) v += sums[i][rr][cc];
         if (a.parts > 1) a.ws[((int64_t)blockIdx.y * a.n + r) * a.K + c] = v;
         else store_margin(a.Z, a.zdtype, r * a.ldz + c, v);
+    }
+}
+
+// More rows: a wave takes 16 RT rows and 64 classes, WM x WN waves side by side share the rows' blocks through LDS, and WK
+// such groups take a stretch of the features each and add their sums in order.  Two buffers of rows per group; a row's sixteen
+// chunks of 16 bytes are exchanged by the row's number in its tile of sixteen, so that the sixteen lanes that read one chunk
+// of sixteen rows meet all banks.  fp32 rows are split on their way into LDS.  The weights come straight from memory in their
+// operands' order, one block ahead.  Each group's products are summed in registers of their own and scaled from there.
+template <typename T, int GROUP, int RT, int WM, int WN, int WK>
+__global__ __launch_bounds__(WM *WN *WK *WAVE) void q4_tile_kernel(Q4Args a)
+{
+    typedef typename Rows<T>::Op Op;
+    constexpr int PIECES = Rows<T>::PIECES, PER = GROUP / 32, GROUPS = BLOCK / GROUP, OT = 4;
+    constexpr int SIDE = WM * WN * WAVE, ROWS = 16 * RT * WM, LOADS = ROWS * 16 / SIDE, CLASSES = WN * OT * TILE;
+    constexpr int BUFFER = PIECES * ROWS * 16;                         // chunks of a buffer
+    static_assert(LOADS * SIDE == ROWS * 16 && LOADS >= 1, "whole rounds of the chunks");
+    static_assert(WK == 1 || ROWS * CLASSES * 4 <= 2 * WK * BUFFER * 16, "a group's sums fit the buffers");
+    typedef typename ScaleWord<GROUPS>::type Scales;
+    constexpr int LINE = OT * TILE + 4, OUT = TILE * LINE / 4;         // a tile row of a wave's results on their way out, in chunks
+    __shared__ Raw lds[2 * WK * BUFFER > WM * WN * OUT ? 2 * WK * BUFFER : WM * WN * OUT];
+    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), o = lane & 15, g = lane >> 4;
+    const int wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN, side = threadIdx.x - wk * SIDE;
+    const int blocks = (int)((a.p + BLOCK - 1) / BLOCK), tiles = (int)((a.K + TILE - 1) / TILE), whole = (int)(a.p / BLOCK);
+    const int64_t r0 = (int64_t)blockIdx.x * ROWS;
+    const int t0 = blockIdx.z * (WN * OT) + wn * OT;
+    const int shares = a.parts * WK, mine = blockIdx.y * WK + wk;
+    const int first = (int)((int64_t)blocks * mine / shares), last = (int)((int64_t)blocks * (mine + 1) / shares);
+    const int rounds = (blocks + shares - 1) / shares;                 // of the group with most blocks
+
+    const Raw *w[OT];
+    const Scales *sc[OT];
+#pragma unroll
+    for (int ot = 0; ot < OT; ++ot) {
+        const int64_t t = t0 + ot < tiles ? t0 + ot : tiles - 1;
+        w[ot] = (const Raw *)a.packed + (t * blocks + first) * WAVE;
+        sc[ot] = (const Scales *)a.scales + (t * blocks + first) * TILE;
+    }
+    // the thread's chunks: row (i SIDE + side) / 16, chunk side % 16
+    const int chunk = side & 15, row = side >> 4;
+    const T *x[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int64_t r = r0 + row + i * (SIDE / 16);
+        x[i] = (const T *)a.X + (r < a.n ? r : a.n - 1) * a.ldx + chunk * 8;
+    }
+    constexpr int WORDS = sizeof(T) / 2;                               // 16-byte loads of a chunk's features
+    Raw xr[LOADS][WORDS], q[OT];
+    Scales s[OT];
+    auto fetch_rows = [&](int b, int i) {
+#pragma unroll
+        for (int h = 0; h < WORDS; ++h) xr[i][h] = *(const RawAt2 *)(x[i] + (int64_t)b * BLOCK + h * 4);
+    };
+    auto fetch_weights = [&](int b, int ot) {
+        q[ot] = (w[ot] + (int64_t)(b - first) * WAVE)[lane];
+        s[ot] = (sc[ot] + (int64_t)(b - first) * TILE)[o];
+    };
+    // where the thread's chunks go in a buffer, and where the lane's operands are
+    int put[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int rr = row + i * (SIDE / 16);
+        put[i] = rr * 16 + (chunk ^ (rr & 15));
+    }
+    float acc[OT][RT][4];
+#pragma unroll
+    for (int ot = 0; ot < OT; ++ot)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[ot][rt][i] = 0.0f;
+    // what is fetched behind the end (the last whole block of rows, the last block of weights) is not used
+    const int start = first < blocks ? first : blocks - 1;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) fetch_rows(start < whole ? start : whole - 1, i);
+#pragma unroll
+    for (int ot = 0; ot < OT; ++ot) fetch_weights(start, ot);
+    for (int i0 = 0; i0 < rounds; ++i0) {
+        const int b = first + i0;
+        Raw *buf = lds + (2 * wk + (i0 & 1)) * BUFFER;
+        if (b == whole) {                                              // the features end inside this block
+            const int left = (int)(a.p - (int64_t)b * BLOCK) - chunk * 8;
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                T tail[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) tail[e] = e < left ? x[i][(int64_t)b * BLOCK + e] : zero_of<T>();
+                __builtin_memcpy(xr[i], tail, sizeof(tail));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            Op op[PIECES];
+            Rows<T>::operand(xr[i], op);
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) buf[k * ROWS * 16 + put[i]] = __builtin_bit_cast(Raw, op[k]);
+        }
+        __syncthreads();                                               // the other buffer's readers are behind this too
+        if (b >= last) continue;
+        const Raw *at = buf + (wm * 16 * RT + o) * 16;
+        Op xo[4][RT][PIECES];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int k = 0; k < PIECES; ++k)
+                    xo[j][rt][k] = __builtin_bit_cast(Op, at[(k * ROWS + rt * 16) * 16 + ((4 * j + g) ^ o)]);
+        const int next = b + 1 < blocks ? b + 1 : blocks - 1, next_rows = b + 1 < whole ? b + 1 : whole - 1;
+        // the next block's loads go out between the products: all at once they would hold the wave up for as long as the
+        // products take
+#pragma unroll
+        for (int ot = 0; ot < OT; ++ot) {
+            F4 d[RT];
+            const Raw words = q[ot];
+            const Scales scales = s[ot];
+            fetch_weights(next, ot);
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i)
+                if (i * OT / LOADS == ot) fetch_rows(next_rows, i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Op wo = Rows<T>::codes(words[j]);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    if (j % PER == 0) d[rt] = F4{0, 0, 0, 0};
+#pragma unroll
+                for (int k = PIECES - 1; k >= 0; --k)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) d[rt] = Rows<T>::mul(xo[j][rt][k], wo, d[rt]);
+                if (j % PER == PER - 1) {
+                    const float f = bf16_value((uint16_t)(scales >> (16 * (j / PER))));
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[ot][rt][i] = fmaf(f, d[rt][i], acc[ot][rt][i]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    if constexpr (WK > 1) {
+        // the groups' sums in order: lane-major, so that neither side waits for a bank
+        constexpr int LANES = WM * WN * WAVE;
+        F4 *sums = (F4 *)lds;
+        for (int k = 1; k < WK; ++k) {
+            __syncthreads();                                           // the buffers, or the last group's sums, have been read
+            if (wk == k) {
+#pragma unroll
+                for (int ot = 0; ot < OT; ++ot)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+                        sums[(ot * RT + rt) * LANES + side] = F4{acc[ot][rt][0], acc[ot][rt][1], acc[ot][rt][2], acc[ot][rt][3]};
+            }
+            __syncthreads();
+            if (wk == 0) {
+#pragma unroll
+                for (int ot = 0; ot < OT; ++ot)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const F4 v = sums[(ot * RT + rt) * LANES + side];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[ot][rt][i] += v[i];
+                    }
+            }
+        }
+    }
+    // Results through LDS, sixteen rows of the wave's 64 classes at a time: eight lanes write eight classes each of a row
+    __syncthreads();
+    if (wk) return;
+    float *out = (float *)(lds + (wm * WN + wn) * OUT);
+    const int64_t c = (int64_t)t0 * TILE + (lane & 7) * 8;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int ot = 0; ot < OT; ++ot)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) out[(4 * g + i) * LINE + ot * TILE + o] = acc[ot][rt][i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int rr = h * 8 + (lane >> 3);
+            const int64_t r = r0 + wm * 16 * RT + rt * 16 + rr;
+            const F4 lo = *(const F4 *)(out + rr * LINE + (lane & 7) * 8), hi = *(const F4 *)(out + rr * LINE + (lane & 7) * 8 + 4);
+            const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (r >= a.n || c >= a.K) continue;
+            if (a.parts > 1) store_margins((float *)a.ws + ((int64_t)blockIdx.y * a.n + r) * a.K + c, a.K - c, v);
+            else if (a.zdtype == SSN_F32) store_margins((float *)a.Z + r * a.ldz + c, a.K - c, v);
+            else if (a.zdtype == SSN_F16) store_margins((_Float16 *)a.Z + r * a.ldz + c, a.K - c, v);
+            else store_margins((__bf16 *)a.Z + r * a.ldz + c, a.K - c, v);
+        }
     }
 }
 
@@ -288,14 +567,51 @@ __global__ __launch_bounds__(VEC_BLOCK) void q4_quantize_kernel(const T *W, int6
 
 }  // namespace
 
+// Which kernel serves a call, by its sizes and types alone; figures are for bfloat16 rows and groups of 32 on 256 compute
+// units.
+//   Few rows, one register in four (up to 4 rows), two (8) or all: a wave per tile and stretch of the features while the
+//   tiles are few (4096 x 4096, one row: 4.7 us, four tiles a wave 8.3 us), four tiles a wave, which read the rows' operands
+//   once, when there are many (8192 x 65536: 57 us, one tile a wave 80 us).
+//   More rows: the largest tile that still gives most compute units a workgroup (256 rows, 4096 x 32768 in groups of 128:
+//   128 rows x 256 classes 64 us, 32 x 128 115 us; 128 rows, 4096 x 8192: 32 x 128 21 us, 128 x 256 64 us).
+namespace {
+enum Q4Form : int {
+    Q4_ROWS4, Q4_ROWS4_WIDE, Q4_ROWS8, Q4_ROWS8_WIDE, Q4_ROWS16, Q4_ROWS16_WIDE,       // stream kernel
+    Q4_TILE16, Q4_TILE16_HALF, Q4_TILE32, Q4_TILE64, Q4_TILE64_WIDE, Q4_TILE128         // tile kernel: rows of a workgroup
+};
+int64_t groups_of(int64_t n, int64_t K, int rows, int classes) { return (n + rows - 1) / rows * ((K + classes - 1) / classes); }
+}  // namespace
+
 void q4_plan(int num_cus, Q4Args *a)
 {
-    const int64_t blocks = (a->p + BLOCK - 1) / BLOCK, tiles = (a->K + TILE - 1) / TILE;
-    const int64_t groups = tiles * ((a->n + 63) / 64);
-    int64_t parts = 1;
-    if (groups < num_cus) parts = (num_cus + groups - 1) / groups;
-    const int64_t most = blocks / (Q4_WAVES * 4);                      // four blocks at least for each wave
-    if (parts > most) parts = most;
+    const int64_t blocks = (a->p + BLOCK - 1) / BLOCK, tiles = (a->K + TILE - 1) / TILE, n = a->n, K = a->K;
+    const bool split = a->dtype == SSN_F32;
+    int64_t groups, share = 64;                                        // workgroups, and blocks that keep one busy
+    if (n <= 4) {
+        a->form = tiles >= (split ? 7 : 10) * num_cus / 2 ? Q4_ROWS4_WIDE : Q4_ROWS4;
+        groups = a->form == Q4_ROWS4 ? tiles : tiles / 4;
+    } else if (n <= 8) {
+        a->form = tiles >= (split ? 8 : 10) * num_cus / 2 ? Q4_ROWS8_WIDE : Q4_ROWS8;
+        groups = a->form == Q4_ROWS8 ? tiles / 2 + 1 : tiles / 4;
+    } else if (a->p < BLOCK || (n <= 16 && (!split || tiles < 4 * num_cus))) {
+        a->form = tiles >= (split ? 2 : 3) * num_cus ? Q4_ROWS16_WIDE : Q4_ROWS16;
+        groups = (tiles / 2 + 1) * ((n + 15) / 16);
+    } else if (split) {
+        a->form = groups_of(n, K, 16, 128) >= 2 * num_cus ? Q4_TILE16_HALF : Q4_TILE16;
+        groups = groups_of(n, K, 16, 128);
+    } else {
+        const int64_t enough = 5 * num_cus / 8;
+        a->form = Q4_TILE16;
+        if (n > 64 && groups_of(n, K, 128, 256) >= enough) a->form = Q4_TILE128;
+        else if (n > 32 && groups_of(n, K, 64, 256) >= enough) a->form = Q4_TILE64_WIDE;
+        else if (n > 32 && groups_of(n, K, 64, 128) >= enough) a->form = Q4_TILE64;
+        else if (groups_of(n, K, 32, 128) >= enough) a->form = Q4_TILE32;
+        groups = groups_of(n, K, 16, 128);
+        share = 32;
+    }
+    // so few classes that most compute units would have nothing: parts of the features, joined by a launch of its own
+    int64_t parts = groups < num_cus / 2 ? num_cus / groups : 1;
+    if (parts > blocks / share) parts = blocks / share;
     if (parts > 64) parts = 64;
     a->parts = (int)(parts < 1 ? 1 : parts);
 }
@@ -304,19 +620,41 @@ int64_t q4_workspace(const Q4Args &a) { return a.parts > 1 ? (int64_t)a.parts * 
 
 template <typename T, int GROUP> static void q4_launch(const Q4Args &a, hipStream_t st)
 {
+    constexpr bool SPLIT = sizeof(T) == 4;
     const int64_t tiles = (a.K + TILE - 1) / TILE;
-    auto go = [&](auto rt, auto used, auto ot) {
-        constexpr int RT = decltype(rt)::value, USED = decltype(used)::value, OT = decltype(ot)::value;
-        const dim3 grid((unsigned)((tiles + OT - 1) / OT), (unsigned)a.parts, (unsigned)((a.n + 16 * RT - 1) / (16 * RT)));
-        hipLaunchKernelGGL((q4_stream_kernel<T, GROUP, RT, USED, OT>), grid, dim3(Q4_WAVES * WAVE), 0, st, a);
+    auto stream = [&](auto used, auto ot, auto waves, auto depth) {
+        constexpr int USED = decltype(used)::value, OT = decltype(ot)::value, WAVES = decltype(waves)::value;
+        const dim3 grid((unsigned)((tiles + OT - 1) / OT), (unsigned)a.parts, (unsigned)((a.n + 15) / 16));
+        hipLaunchKernelGGL((q4_stream_kernel<T, GROUP, USED, OT, WAVES, decltype(depth)::value>), grid, dim3(WAVES * WAVE), 0, st, a);
+    };
+    auto tile = [&](auto rt, auto wm, auto wn, auto wk) {
+        constexpr int RT = decltype(rt)::value, WM = decltype(wm)::value, WN = decltype(wn)::value, WK = decltype(wk)::value;
+        const dim3 grid((unsigned)((a.n + 16 * RT * WM - 1) / (16 * RT * WM)), (unsigned)a.parts, (unsigned)((tiles + 4 * WN - 1) / (4 * WN)));
+        hipLaunchKernelGGL((q4_tile_kernel<T, GROUP, RT, WM, WN, WK>), grid, dim3(WM * WN * WK * WAVE), 0, st, a);
     };
     std::integral_constant<int, 1> one;
     std::integral_constant<int, 2> two;
     std::integral_constant<int, 4> four;
-    if (a.n <= 4) go(one, one, one);
-    else if (a.n <= 16) go(one, four, one);
-    else if (a.n <= 32) go(two, four, one);
-    else go(four, four, two);
+    std::integral_constant<int, 8> eight;
+    std::integral_constant<int, SPLIT ? 8 : 4> wide;
+    switch (a.form) {
+    case Q4_ROWS4: stream(one, one, eight, two); return;
+    case Q4_ROWS4_WIDE: stream(one, four, wide, one); return;
+    case Q4_ROWS8: stream(two, two, eight, one); return;
+    case Q4_ROWS8_WIDE: stream(two, four, four, one); return;
+    case Q4_ROWS16: stream(four, two, eight, one); return;
+    case Q4_ROWS16_WIDE: stream(four, four, eight, one); return;
+    case Q4_TILE16: tile(one, one, two, four); return;
+    default: break;
+    }
+    if constexpr (SPLIT) {
+        tile(one, one, two, two);                                      // Q4_TILE16_HALF
+    } else {
+        if (a.form == Q4_TILE32) tile(two, one, two, four);
+        else if (a.form == Q4_TILE64) tile(two, two, two, two);
+        else if (a.form == Q4_TILE64_WIDE) tile(four, one, four, two);
+        else tile(four, two, four, one);
+    }
 }
 
 hipError_t launch_q4_margins(Q4Args &a, void *workspace, hipStream_t st)

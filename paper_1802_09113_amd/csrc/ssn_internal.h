@@ -514,8 +514,8 @@ struct Q4Args {
     void *Z;
     int64_t ldz;
     int32_t dtype, zdtype;
-    // set by q4_plan: parts of the features (partial sums of each in the workspace where there is more than one)
-    int32_t parts;
+    // set by q4_plan: which kernel, and parts of the features (sums of each in the workspace where there is more than one)
+    int32_t form, parts;
     float *ws;
 };
 void q4_plan(int num_cus, Q4Args *a);

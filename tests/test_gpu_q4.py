@@ -142,6 +142,21 @@ def test_margins(dtype, group, n, p, K):
     check_margins(block, X)
 
 
+# as many classes as it takes for each form to serve (256 compute units); odd numbers of rows, features and classes
+@pytest.mark.parametrize("dtype,group,n,p,K", [
+    ("bf16", 32, 1, 300, 20500), ("f16", 64, 3, 1025, 24001), ("f32", 32, 2, 300, 14500), ("bf16", 128, 6, 300, 20500),
+    ("f32", 64, 7, 300, 16500), ("f16", 32, 12, 300, 12500), ("f32", 128, 11, 300, 8300), ("f32", 32, 13, 300, 16500),
+    ("f32", 32, 30, 140, 33001), ("bf16", 32, 100, 300, 5200), ("f16", 128, 40, 300, 20501), ("bf16", 64, 200, 300, 11001),
+    ("f16", 32, 130, 300, 20501), ("bf16", 128, 257, 128, 20480), ("bf16", 32, 150, 127, 2000), ("f32", 32, 40, 100, 700)])
+def test_margins_of_many_classes(dtype, group, n, p, K):
+    rng = np.random.default_rng(n + p + K)
+    block = random_block(p, K, group, rng)
+    X = torch.from_numpy(rng.standard_normal((n, p))).to(F[dtype]).cuda()
+    check_margins(block, X)
+    if dtype != "f32":
+        check_margins(block, X, torch.empty(n, K, device="cuda"))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_margins_of_strided_and_unaligned_rows(dtype):
     """Rows at addresses aligned to one element, NaN between and behind them; results into a wider float32 buffer whose
