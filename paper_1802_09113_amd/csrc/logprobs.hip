@@ -42,7 +42,8 @@ template <typename T> struct Vec {
     static constexpr int E = 16 / sizeof(T);
     typedef typename std::conditional<sizeof(T) == 2, RawAt2, RawAt4>::type RawAt;
     static __device__ __forceinline__ Raw load(const T *p) { return *(const RawAt *)p; }
-    static __device__ __forceinline__ void store(T *p, Raw v) { *(RawAt *)p = v; }
+    // past the caches, which a gradient of any size worth a kernel outgrows: 8192 x 65536 bf16 367 -> 353 us, 1021 x 32003 fp32 57 -> 47 us
+    static __device__ __forceinline__ void store(T *p, Raw v) { __builtin_nontemporal_store(v, (RawAt *)p); }
 };
 
 __device__ __forceinline__ void unpack(Raw r, float (&x)[4], float)
@@ -765,6 +766,33 @@ template <typename A> struct RowGrad {
         if (h != A(0)) w = fma(h, take_max(lp, A(-1e4)) + H, w);
         return -exp_value(lp) * w;
     }
+    // A vector of them.  16-bit results take one multiply-add for the exponent: with k = c M rounded and r = c M - k, which is
+    // exact, p = 2^(c z - k) f with f = 2^(-r - c L), a factor of the row; what is left of p's error, |c (z - M)| 2^-24, is
+    // far below their rounding.  Where c z could overflow, at() does it.
+    template <typename T, int E> __device__ __forceinline__ void values(A (&x)[E]) const
+    {
+        if constexpr (sizeof(T) == 2) {
+            if (fabsf(M) < 1e38f) {
+                const float c = 1.44269504f, k = M * c, r = fmaf(M, c, -k), f = __builtin_amdgcn_exp2f(-fmaf(L, c, r));
+                if (h == 0.0f) {
+                    const float w = -G * f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], c, -k)) * w;
+                } else {
+                    // G + h (log p + H) with log p = (d - r) / c - L
+                    const float slope = -f * h * (1.0f / c), base = -f * fmaf(h, H - L - r * (1.0f / c), G);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float d = fmaf(x[e], c, -k);
+                        x[e] = __builtin_amdgcn_exp2f(d) * fmaf(slope, fmaxf(d, -1e4f), base);
+                    }
+                }
+                return;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = at(x[e]);
+    }
 };
 // given class y's weight: none for padding and for a class without probability, NaN for an index that is no class
 template <typename A> __device__ __forceinline__ A given_weight(const LogprobsArgs &a, int64_t at, int y)
@@ -774,33 +802,29 @@ template <typename A> __device__ __forceinline__ A given_weight(const LogprobsAr
     return ((const A *)a.logp)[at] == minus_inf(A()) ? A(0) : ((const A *)a.dlogp)[at];
 }
 
-template <typename T> __global__ __launch_bounds__(VEC_BLOCK) void logprobs_grad_wide_kernel(LogprobsArgs a)
+// WAVES waves walk a stretch of a row, GRAD_AHEAD loads of 16 bytes per thread in flight; the row's statistics and given
+// classes are fetched behind the first of them.
+constexpr int GRAD_AHEAD = 2;
+template <typename T, int WAVES> __global__ __launch_bounds__(WAVES *WAVE) void logprobs_grad_wide_kernel(LogprobsArgs a)
 {
     typedef typename Acc<T>::type A;
-    constexpr int E = Vec<T>::E, U = 2, TILE = VEC_BLOCK * E * U;
-    const int lane = threadIdx.x & (WAVE - 1);
-    const int64_t c0 = (int64_t)blockIdx.x * TILE;
+    constexpr int E = Vec<T>::E, STEP = WAVES * WAVE * E, AHEAD = GRAD_AHEAD;
+    const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int64_t first = (int64_t)blockIdx.x * a.per_wave, end = first + a.per_wave < a.width ? first + a.per_wave : a.width;
     for (int64_t row = blockIdx.y; row < a.n; row += gridDim.y) {
-        const T *z = (const T *)a.Z + row * a.ldz;
+        Stretch<T> in;
+        in.z = (const T *)a.Z + row * a.ldz;
+        in.mask = a.allowed ? a.allowed + row * a.ld_allowed : nullptr;
+        in.first = first, in.end = end;
         T *dz = (T *)a.dZ + row * a.lddz;
-        const uint32_t *mask = a.allowed ? a.allowed + row * a.ld_allowed : nullptr;
-        Raw raw[U];
-        uint32_t word[U];
+        Raw raw[AHEAD];
+        uint32_t word[AHEAD];
+        auto fetch = [&](int64_t c0, int u) {
+            const int64_t c1 = c0 + u * STEP + wave * WAVE * E;
+            in.load(c1, lane, c1 + WAVE * E <= end, raw[u], word[u]);
+        };
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t c = c0 + (u * VEC_BLOCK + threadIdx.x) * E;
-            raw[u] = Raw{0, 0, 0, 0};
-            word[u] = 0xffffffffu;
-            if (c + E <= a.width) {
-                raw[u] = Vec<T>::load(z + c);
-            } else if (c < a.width) {
-                T tail[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) tail[e] = z[c + e < a.width ? c + e : a.width - 1];
-                raw[u] = __builtin_bit_cast(Raw, tail);
-            }
-            if (mask && c < a.width) word[u] = mask[c >> 5];
-        }
+        for (int u = 0; u < AHEAD; ++u) fetch(first, u);
         int y = -1;
         A gy = A(0);
         if (lane < a.m) {
@@ -810,28 +834,41 @@ template <typename T> __global__ __launch_bounds__(VEC_BLOCK) void logprobs_grad
         RowGrad<A> w;
         w.load(a, row);
         w.G += wave_sum(gy);
+        for (int64_t c0 = first; c0 < end; c0 += AHEAD * STEP) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t cw = c0 + (u * VEC_BLOCK + (threadIdx.x - lane)) * E;     // the wave's stretch
-            if (cw >= a.width) break;
-            const int64_t c = cw + lane * E;
-            A x[E];
-            unpack(raw[u], x, T());
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t c1 = c0 + u * STEP + wave * WAVE * E;    // the wave's columns
+                if (c1 >= end) break;
+                const bool whole = c1 + WAVE * E <= end;
+                const int64_t c = c1 + lane * E;
+                A x[E];
+                unpack(raw[u], x, T());
+                const uint32_t bits = in.mask ? word[u] >> (c & 31) : 0xffffffffu;
+                if (c0 + AHEAD * STEP < end) fetch(c0 + AHEAD * STEP, u);
+                if (w.empty) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = w.empty || !((word[u] >> ((c & 31) + e)) & 1u) ? A(0) : w.at(x[e]);
-            for (unsigned long long b = __ballot(gy != A(0) && y >= cw && y < cw + WAVE * E); b; b &= b - 1) {
-                const int from = __ffsll(b) - 1;
-                const int64_t yy = __builtin_amdgcn_readlane(y, from);
-                const A g = at_lane(gy, from);
+                    for (int e = 0; e < E; ++e) x[e] = A(0);
+                } else {
+                    w.template values<T>(x);
+                    if (in.mask) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[e] += c + e == yy ? g : A(0);
-            }
-            if (c + E <= a.width) {
-                Vec<T>::store(dz + c, pack(x, T()));
-            } else {
+                        for (int e = 0; e < E; ++e) x[e] = (bits >> e) & 1u ? x[e] : A(0);
+                    }
+                }
+                for (unsigned long long b = __ballot(gy != A(0) && y >= c1 && y < c1 + WAVE * E); b; b &= b - 1) {
+                    const int from = __ffsll(b) - 1;
+                    const int64_t yy = __builtin_amdgcn_readlane(y, from);
+                    const A g = at_lane(gy, from);
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (c + e < a.width) dz[c + e] = (T)x[e];
+                    for (int e = 0; e < E; ++e) x[e] += c + e == yy ? g : A(0);
+                }
+                if (whole || c + E <= end) {
+                    Vec<T>::store(dz + c, pack(x, T()));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (c + e < end) dz[c + e] = (T)x[e];
+                }
             }
         }
     }
@@ -981,8 +1018,19 @@ hipError_t launch_logprobs_grad(int dtype, const LogprobsArgs &a, hipStream_t st
             });
             return;
         }
-        constexpr int TILE = VEC_BLOCK * Vec<T>::E * 2;
-        hipLaunchKernelGGL((logprobs_grad_wide_kernel<T>), row_grid((a.width + TILE - 1) / TILE, a.n), dim3(VEC_BLOCK), 0, st, a);
+        // A short row is one wave's.  A workgroup takes two rounds of loads, the second of which is on its way while the first
+        // is worked on (8192 x 65536 bf16: one round 457 us, two 353 us, four 391 us), or one where two would leave compute
+        // units without work (4 x 32000 fp32: 5.5 and 6.3 us).
+        LogprobsArgs b = a;
+        auto go = [&](auto waves) {
+            constexpr int W = decltype(waves)::value;
+            const int64_t round = W * WAVE * Vec<T>::E * GRAD_AHEAD;
+            b.per_wave = a.n * ((a.width + 2 * round - 1) / (2 * round)) >= 1024 ? 2 * round : round;
+            hipLaunchKernelGGL((logprobs_grad_wide_kernel<T, W>), row_grid((a.width + b.per_wave - 1) / b.per_wave, a.n), dim3(W * WAVE),
+                               0, st, b);
+        };
+        if (a.width * (int64_t)sizeof(T) <= 4096) go(std::integral_constant<int, 1>());
+        else go(std::integral_constant<int, 4>());
     });
 }
 

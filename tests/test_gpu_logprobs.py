@@ -153,7 +153,7 @@ def some_labels(n, m, C, rng):
 # one class; each border between the forms (512 classes; 8 and 16 wave loads of 16 bytes; vectors that end inside a row);
 # rows split over workgroups (few rows) and not (many)
 SIZES = [(1, 1), (3, 2), (300, 7), (65, 8), (64, 9), (5, 64), (3, 65), (9, 512), (3, 513), (2, 517), (1, 1000), (3, 2047), (5, 2049),
-         (2, 4096), (2, 4100), (7, 4099), (3, 8191), (1, 16385), (1, 32003), (600, 9001), (300, 9001), (2100, 3001), (2, 131077)]
+         (2, 4096), (2, 4100), (7, 4099), (3, 8191), (1, 16385), (70, 300), (1100, 900), (1, 32003), (600, 9001), (300, 9001), (2100, 3001), (2, 131077)]
 
 
 @pytest.mark.parametrize("n,C", SIZES)
