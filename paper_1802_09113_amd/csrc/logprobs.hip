@@ -185,10 +185,30 @@ template <typename A> __device__ __forceinline__ A wave_sum(A x)
     x += dpp_or_none<0x143, 0xc>(x);
     return at_lane(x, 63);
 }
-template <typename A> __device__ __forceinline__ A sum_over(A x, int lanes)
+// The value of the lane that is O apart in a group of 2 O lanes whose halves hold one value each (O = 1, 2, 4, ... in turn):
+// exchanges of lanes inside rows of sixteen, through LDS beyond
+template <int O> __device__ __forceinline__ int across(int x)
 {
-    for (int o = lanes / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, WAVE);
-    return x;
+    if (O == 1) return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, false);       // lanes 1 0 3 2
+    if (O == 2) return __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, false);       // lanes 2 3 0 1
+    if (O == 4) return __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false);      // halves of a row mirrored
+    if (O == 8) return __builtin_amdgcn_update_dpp(0, x, 0x140, 0xf, 0xf, false);      // rows mirrored
+    return __shfl_xor(x, O, WAVE);
+}
+template <int O> __device__ __forceinline__ float across(float x) { return __uint_as_float((uint32_t)across<O>((int)__float_as_uint(x))); }
+template <int O> __device__ __forceinline__ double across(double x)
+{
+    const long long b = __double_as_longlong(x);
+    const uint32_t lo = (uint32_t)across<O>((int)b);
+    return __longlong_as_double(((long long)across<O>((int)(b >> 32)) << 32) | lo);
+}
+// f<O>() for O = 1, 2, ..., G / 2
+template <int G, int O = 1, typename F> __device__ __forceinline__ void each_step(F f)
+{
+    if constexpr (O < G) {
+        f(std::integral_constant<int, O>());
+        each_step<G, 2 * O>(f);
+    }
 }
 
 // ---- the running statistics of a row ---------------------------------------------------------------------------------
@@ -497,9 +517,9 @@ __global__ __launch_bounds__(WAVES *WAVE) void logprobs_wide_kernel(LogprobsArgs
         // the lane's second and third largest maximum of a vector (acc.mx is the largest), and the steps of the first two
         A v2 = minus_inf(A()), v3 = minus_inf(A());
         int at1 = 0, at2 = 0;
+        Raw raw[AHEAD];
+        uint32_t word[AHEAD];
         for (int64_t c1 = in.first; c1 < in.end; c1 += AHEAD * STEP) {
-            Raw raw[AHEAD];
-            uint32_t word[AHEAD];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) in.load(c1 + u * STEP, lane, c1 + (u + 1) * STEP <= in.end, raw[u], word[u]);
 #pragma unroll
@@ -574,23 +594,32 @@ __global__ __launch_bounds__(WAVES *WAVE) void logprobs_wide_kernel(LogprobsArgs
                     }
             };
             if (v1 >= tau) {
-                Raw raw, more;
-                uint32_t word, bits;
+                Raw r1, r2;
+                uint32_t w1, w2;
                 A x[E];
                 if (v3 < tau) {                                        // all of the lane's are in one vector or two
                     const int64_t col = in.first + lane * E;
-                    in.load_any(col + at1, raw, word);
-                    if (v2 >= tau) in.load_any(col + at2, more, bits);
-                    in.get(col + at1, raw, word, false, x);
+                    if (a.per_wave <= AHEAD * STEP) {                  // and those are still here
+                        r1 = r2 = raw[0], w1 = w2 = word[0];
+#pragma unroll
+                        for (int u = 1; u < AHEAD; ++u) {
+                            if (at1 == u * STEP) r1 = raw[u], w1 = word[u];
+                            if (at2 == u * STEP) r2 = raw[u], w2 = word[u];
+                        }
+                    } else {
+                        in.load_any(col + at1, r1, w1);
+                        if (v2 >= tau) in.load_any(col + at2, r2, w2);
+                    }
+                    in.get(col + at1, r1, w1, false, x);
                     put(col + at1, x);
                     if (v2 >= tau) {
-                        in.get(col + at2, more, bits, false, x);
+                        in.get(col + at2, r2, w2, false, x);
                         put(col + at2, x);
                     }
                 } else {
                     for (int64_t col = in.first + lane * E; col < in.end; col += STEP) {
-                        in.load_any(col, raw, word);
-                        in.get(col, raw, word, false, x);
+                        in.load_any(col, r1, w1);
+                        in.get(col, r1, w1, false, x);
                         put(col, x);
                     }
                 }
@@ -666,15 +695,20 @@ template <typename T, bool TOP> __global__ __launch_bounds__(TOP ? VEC_BLOCK : W
         }
         if (TOP) {
             const int64_t at = row * a.parts * a.k;
-            const A tau = wave_max(lane < a.parts ? ((const A *)a.ws_val)[at + lane * a.k + a.k - 1] : minus_inf(A()));
+            const int N = a.parts * a.k;
+            A kth = minus_inf(A()), v = minus_inf(A());
+            int id = -1;
+            if (lane < a.parts) kth = ((const A *)a.ws_val)[at + lane * a.k + a.k - 1];
+            if (threadIdx.x < N) v = ((const A *)a.ws_val)[at + threadIdx.x], id = a.ws_id[at + threadIdx.x];
             if (threadIdx.x == 0) sh_count = 0;
             if (threadIdx.x < WAVE) sh_slot[lane] = minus_inf(A()), sh_slot_id[lane] = -1;
             __syncthreads();
-            for (int i = threadIdx.x; i < a.parts * a.k; i += VEC_BLOCK) {
-                const A v = ((const A *)a.ws_val)[at + i];
+            const A tau = wave_max(kth);
+            for (int i = threadIdx.x; i < N; i += VEC_BLOCK) {
+                if (i >= VEC_BLOCK) v = ((const A *)a.ws_val)[at + i], id = a.ws_id[at + i];
                 if (v >= tau && v > minus_inf(A())) {
                     const int slot = atomicAdd(&sh_count, 1);
-                    sh_val[slot] = v, sh_id[slot] = a.ws_id[at + i];
+                    sh_val[slot] = v, sh_id[slot] = id;
                 }
             }
             __syncthreads();
@@ -698,20 +732,29 @@ template <typename T, int G> __global__ __launch_bounds__(VEC_BLOCK) void logpro
         const int64_t row = base + threadIdx.x / G;
         const bool live = row < a.n;                                   // idle lanes stay for the exchanges below
         A x[R];
+        const T *z = (const T *)a.Z + (live ? row : 0) * a.ldz + g;
+        T raw[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) raw[r] = g + r * G < a.width ? z[r * G] : (T)0.0f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) x[r] = g + r * G < a.C ? (A)raw[r] : minus_inf(A());        // 0: the reference class
+        if (a.allowed) {
+            const uint32_t *mask = a.allowed + (live ? row : 0) * a.ld_allowed;
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (g + r * G < a.C && !allowed_bit(mask, g + r * G)) x[r] = minus_inf(A());
+        }
         Stat<A> q;
         q.init();
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int c = g + r * G;
-            x[r] = live && c < a.C ? margin_of<T>(a, row, c) : minus_inf(A());
-        }
-#pragma unroll
         for (int r = 0; r < R; ++r) q.M = take_max(q.M, x[r]);
-        for (int o = G / 2; o > 0; o >>= 1) q.M = take_max(q.M, __shfl_xor(q.M, o, WAVE));
+        each_step<G>([&](auto o) { q.M = take_max(q.M, across<decltype(o)::value>(q.M)); });
 #pragma unroll
         for (int r = 0; r < R; ++r) q.add(x[r]);
-        q.s = sum_over(q.s, G);
-        q.t = sum_over(q.t, G);
+        each_step<G>([&](auto o) {
+            q.s += across<decltype(o)::value>(q.s);
+            q.t += across<decltype(o)::value>(q.t);
+        });
         const Answer<A> w(q);
         if (live && g == 0) {
             if (a.maxpart) ((A *)a.maxpart)[row] = w.maxpart();
@@ -723,17 +766,19 @@ template <typename T, int G> __global__ __launch_bounds__(VEC_BLOCK) void logpro
             ((A *)a.logp)[row * a.m + i] =
                 y < 0 ? A(0) : y >= a.C ? nan_of(A()) : w.logp(margin_of<T>(a, row, y));
         }
-        for (int i = 0; i < a.k; ++i) {                                // the largest margin left, the lowest class first
-            A v = minus_inf(A());
+        for (int i = 0; i < a.k; ++i) {                                // the largest margin left, then the lowest class with it
+            A v = x[0];
+#pragma unroll
+            for (int r = 1; r < R; ++r) v = take_max(v, x[r]);
+            each_step<G>([&](auto o) { v = take_max(v, across<decltype(o)::value>(v)); });
             int id = -1;
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-                if (x[r] > v) v = x[r], id = g + r * G;
-            for (int o = G / 2; o > 0; o >>= 1) {
-                const A ov = __shfl_xor(v, o, WAVE);
-                const int oid = __shfl_xor(id, o, WAVE);
-                if (ov > v || (ov == v && (unsigned)oid < (unsigned)id)) v = ov, id = oid;
-            }
+            for (int r = R - 1; r >= 0; --r) id = x[r] == v ? g + r * G : id;
+            id = v > minus_inf(A()) ? id : -1;
+            each_step<G>([&](auto o) {
+                const int oid = across<decltype(o)::value>(id);
+                id = (unsigned)oid < (unsigned)id ? oid : id;
+            });
 #pragma unroll
             for (int r = 0; r < R; ++r) x[r] = id == g + r * G ? minus_inf(A()) : x[r];
             if (live && g == 0) {
