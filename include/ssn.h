@@ -71,7 +71,7 @@ enum {
     SSN_E_HIP = -6,           /* a HIP runtime call failed                                       */
     SSN_E_NONFINITE = -7,     /* objective evaluated to NaN/Inf                                  */
     SSN_E_UNSUPPORTED = -8,   /* shape outside the supported range (e.g. C too large)            */
-    SSN_E_TOO_LARGE = -9      /* ssn_hessvec_static: the problem needs more than the fixed workspace */
+    SSN_E_TOO_LARGE = -9      /* the problem needs more than the workspace (fixed, or given)      */
 };
 
 /* Problem description.  Copied by ssn_create; the arrays it points to are borrowed. */
@@ -332,7 +332,7 @@ typedef struct {
  * the allowed classes and L = log sum_c e^{z_c - M} (eq. (8), (9), M without the paper's lower bound of zero):
  *   logp     [dev] n x m: (z_y - M) - L for the given classes y
  *   maxpart  [dev, nullable] n: M            logpart [dev, nullable] n: L
- *   entropy  [dev, nullable] n: -sum_c p_c log p_c
+ *   entropy  [dev, nullable] n: -sum_c p_c log p_c, all four of type A, as top_logp
  *   top_ids  [dev] n x k int32, top_logp [dev] n x k: the k largest margins in descending order, equal ones by ascending
  *            class
  * What is held at a class that is not allowed is not used; such a class counts as a margin of -inf.
@@ -388,7 +388,7 @@ int ssn_q4_quantize(const ssn_q4 *block, int32_t dtype, const void *W, int64_t s
  * zdtype: X's or SSN_F32; both aligned to an element.  Products are exact, sums in fp32, rounded once to Z's type; the
  * order of the sums depends on the sizes only, also on n.  Z must not overlap X.  n = 0: nothing is done.  workspace [dev],
  * 4-byte aligned, of at least the size that ssn_q4_margins_workspace stores in *bytes for the same sizes (often 0; then it
- * may be NULL).  Returns SSN_OK, SSN_E_INVALID_ARG, SSN_E_UNSUPPORTED (n of 2^20 or more, SSN_F64), SSN_E_TOO_LARGE
+ * may be NULL).  Returns SSN_OK, SSN_E_INVALID_ARG, SSN_E_UNSUPPORTED (n of 2^19 or more, SSN_F64), SSN_E_TOO_LARGE
  * (workspace too small) or SSN_E_HIP. */
 int ssn_q4_margins(const ssn_q4 *block, int32_t dtype, int64_t n, const void *X, int64_t ldx, int32_t zdtype, void *Z,
                    int64_t ldz, void *workspace, int64_t workspace_bytes, void *stream);

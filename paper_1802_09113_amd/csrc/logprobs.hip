@@ -7,6 +7,10 @@
 // the row: every lane keeps (M, s, t) of what it has seen and rescales s and t when its M grows; pairs are joined the same
 // way across lanes, waves and workgroups.  s is NaN exactly when a margin is NaN or +inf, and 0 exactly when no class is
 // left (the largest margin contributes e^0 = 1).  All of it in fp32 for fp32, fp16 and bf16 margins, in fp64 for fp64.
+//
+// What bounds it: memory on many long rows (8192 x 65536 bf16, one label: 179 us, 6.0 TB/s; the vector units are 60 % busy
+// with some nine instructions a margin), the vector units where a row is one workgroup's and alternatives are asked for, and
+// launch and latency on single rows (32000 fp32, five alternatives: 8.7 us a call, the kernel 6 to 9 us of it).
 #include "ssn_internal.h"
 #include "ssn_math.h"
 

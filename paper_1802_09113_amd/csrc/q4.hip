@@ -11,6 +11,10 @@
 // (lane / 16, lane % 16): word j of them holds features 128 b + 32 j + 8 g + 0..7 of class 16 t + o, which is lane (g, o)'s
 // share of the right operand of one 16x16x32 matrix instruction.  A wave reads the block with one load of 16 bytes per
 // lane; one, two or four matrix instructions in a row lie inside a group.
+//
+// What bounds it: for few rows the stream of codes and scales (one row, 8192 x 65536, groups of 32: 302 MB in 57 us, 5.3 TB/s),
+// for many the matrix cores (256 f16 rows, 4096 x 32768, groups of 128: 64 us, 1070 TFLOP/s, where a library product of
+// plain f16 matrices reaches 1160), and in groups of 32 the vector units that scale every group's sums (81 us).
 #include "ssn_internal.h"
 
 #include <type_traits>
@@ -312,8 +316,10 @@ __global__ __launch_bounds__(WM *WN *WK *WAVE) void q4_tile_kernel(Q4Args a)
     const int lane = threadIdx.x & (WAVE - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), o = lane & 15, g = lane >> 4;
     const int wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN, side = threadIdx.x - wk * SIDE;
     const int blocks = (int)((a.p + BLOCK - 1) / BLOCK), tiles = (int)((a.K + TILE - 1) / TILE), whole = (int)(a.p / BLOCK);
-    const int64_t r0 = (int64_t)blockIdx.x * ROWS;
-    const int t0 = blockIdx.z * (WN * OT) + wn * OT;
+    // workgroups that share weights are neighbours
+    const unsigned row_groups = (unsigned)((a.n + ROWS - 1) / ROWS);
+    const int64_t r0 = (int64_t)(blockIdx.x % row_groups) * ROWS;
+    const int t0 = blockIdx.x / row_groups * (WN * OT) + wn * OT;
     const int shares = a.parts * WK, mine = blockIdx.y * WK + wk;
     const int first = (int)((int64_t)blocks * mine / shares), last = (int)((int64_t)blocks * (mine + 1) / shares);
     const int rounds = (blocks + shares - 1) / shares;                 // of the group with most blocks
@@ -629,7 +635,8 @@ template <typename T, int GROUP> static void q4_launch(const Q4Args &a, hipStrea
     };
     auto tile = [&](auto rt, auto wm, auto wn, auto wk) {
         constexpr int RT = decltype(rt)::value, WM = decltype(wm)::value, WN = decltype(wn)::value, WK = decltype(wk)::value;
-        const dim3 grid((unsigned)((a.n + 16 * RT * WM - 1) / (16 * RT * WM)), (unsigned)a.parts, (unsigned)((tiles + 4 * WN - 1) / (4 * WN)));
+        const int64_t groups = (a.n + 16 * RT * WM - 1) / (16 * RT * WM) * ((tiles + 4 * WN - 1) / (4 * WN));
+        const dim3 grid((unsigned)groups, (unsigned)a.parts);
         hipLaunchKernelGGL((q4_tile_kernel<T, GROUP, RT, WM, WN, WK>), grid, dim3(WM * WN * WK * WAVE), 0, st, a);
     };
     std::integral_constant<int, 1> one;

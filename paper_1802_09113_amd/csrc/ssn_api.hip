@@ -11,6 +11,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -833,7 +834,7 @@ const char *ssn_strerror(int status)
     case SSN_E_HIP: return "HIP runtime error";
     case SSN_E_NONFINITE: return "non-finite objective";
     case SSN_E_UNSUPPORTED: return "unsupported shape";
-    case SSN_E_TOO_LARGE: return "problem exceeds the fixed workspace of ssn_hessvec_static";
+    case SSN_E_TOO_LARGE: return "workspace too small for the problem";
     default: return "unknown status";
     }
 }
@@ -2110,6 +2111,13 @@ int current_cus(int *cus)
 
 int elem_size(int32_t dtype) { return dtype == SSN_F64 ? 8 : dtype == SSN_F32 ? 4 : dtype == SSN_F16 || dtype == SSN_BF16 ? 2 : 0; }
 bool aligned_to(const void *q, size_t bytes) { return ((uintptr_t)q & (bytes - 1)) == 0; }
+// statistics of rows of `dtype`, nullable
+bool stats_aligned(int32_t dtype, std::initializer_list<const void *> stats)
+{
+    for (const void *q : stats)
+        if (!aligned_to(q, dtype == SSN_F64 ? 8 : 4)) return false;
+    return true;
+}
 
 // the sizes of an ssn_rows
 int rows_sizes(const ssn_rows *r, LogprobsArgs *a)
@@ -2134,6 +2142,7 @@ int rows_data(const ssn_rows *r, LogprobsArgs *a)
     if (!a->n) return SSN_OK;
     if (!r->Z || r->ldz < a->width || !aligned_to(r->Z, elem_size(r->dtype)) || (r->m && !r->labels)) return SSN_E_INVALID_ARG;
     if (r->allowed && r->ld_allowed != 0 && r->ld_allowed < (r->C + 31) / 32) return SSN_E_INVALID_ARG;
+    if (!aligned_to(r->allowed, 4) || !aligned_to(r->labels, 4)) return SSN_E_INVALID_ARG;
     a->Z = r->Z;
     a->ldz = r->ldz;
     a->allowed = r->allowed;
@@ -2156,7 +2165,7 @@ int q4_rows(const ssn_q4 *b, int32_t dtype, int64_t n, Q4Args *a)
 {
     SSN_TRY(q4_sizes(b, a));
     if (n < 0 || !elem_size(dtype)) return SSN_E_INVALID_ARG;
-    if (dtype == SSN_F64 || n >= (int64_t)1 << 20) return SSN_E_UNSUPPORTED;
+    if (dtype == SSN_F64 || n >= (int64_t)1 << 19) return SSN_E_UNSUPPORTED;
     a->dtype = dtype;
     a->n = n;
     return SSN_OK;
@@ -2192,7 +2201,8 @@ int ssn_logprobs(const ssn_rows *r, void *logp, void *maxpart, void *logpart, vo
     LogprobsArgs a;
     SSN_TRY(rows_data(r, &a));
     if (!a.n) return SSN_OK;
-    if ((a.m && !logp) || (a.k && (!top_ids || !top_logp))) return SSN_E_INVALID_ARG;
+    if ((a.m && !logp) || (a.k && (!top_ids || !top_logp)) || !aligned_to(top_ids, 4)) return SSN_E_INVALID_ARG;
+    if (!stats_aligned(r->dtype, {logp, maxpart, logpart, entropy, top_logp})) return SSN_E_INVALID_ARG;
     a.logp = logp;
     a.maxpart = maxpart;
     a.logpart = logpart;
@@ -2216,6 +2226,7 @@ int ssn_logprobs_grad(const ssn_rows *r, const void *logp, const void *maxpart, 
     if (!a.n) return SSN_OK;
     if (!maxpart || !logpart || !dZ || lddz < a.width || !aligned_to(dZ, elem_size(r->dtype))) return SSN_E_INVALID_ARG;
     if ((a.m && (!logp || !dlogp)) || (dentropy && !entropy) || (dZ == r->Z && lddz != r->ldz)) return SSN_E_INVALID_ARG;
+    if (!stats_aligned(r->dtype, {logp, maxpart, logpart, entropy, dlogp, dlse, dentropy})) return SSN_E_INVALID_ARG;
     a.logp = const_cast<void *>(logp);
     a.maxpart = const_cast<void *>(maxpart);
     a.logpart = const_cast<void *>(logpart);

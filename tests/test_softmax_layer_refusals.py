@@ -25,11 +25,14 @@ def test_log_probabilities():
     assert L.ssn_logprobs_workspace(None, ctypes.byref(size)) == SSN_E_INVALID_ARG
     assert L.ssn_logprobs_workspace(ctypes.byref(rows()), None) == SSN_E_INVALID_ARG
     for bad in (dict(n=-1), dict(C=0), dict(C=1, reference=1), dict(reference=2), dict(dtype=4), dict(dtype=-1), dict(Z=None), dict(Z=66),
-                dict(ldz=99), dict(m=-1), dict(k=-1), dict(C=3, k=4), dict(labels=None), dict(allowed=64, ld_allowed=3)):
+                dict(ldz=99), dict(m=-1), dict(k=-1), dict(C=3, k=4), dict(labels=None), dict(labels=66), dict(allowed=64, ld_allowed=3), dict(allowed=66, ld_allowed=4), dict(allowed=64, ld_allowed=-4)):
         assert forward(rows(**bad)) == SSN_E_INVALID_ARG, bad
     for bad in (dict(C=1 << 31), dict(n=1 << 31), dict(m=65), dict(k=65)):
         assert forward(rows(**bad)) == SSN_E_UNSUPPORTED, bad
     assert forward(rows(), logp=None) == SSN_E_INVALID_ARG
+    assert forward(rows(), logp=66) == SSN_E_INVALID_ARG
+    assert forward(rows(dtype=binding.SSN_F64), logp=68) == SSN_E_INVALID_ARG
+    assert forward(rows(k=2), k_out=66) == SSN_E_INVALID_ARG
     assert forward(rows(k=2), k_out=None) == SSN_E_INVALID_ARG
     assert forward(rows(n=0, Z=None, labels=None)) == SSN_OK
     size.value = 5
@@ -43,7 +46,7 @@ def test_their_gradient():
         return L.ssn_logprobs_grad(ctypes.byref(d), P(logp), P(maxpart), P(logpart), P(entropy), P(dlogp), P(dlse), P(dentropy), P(dZ), ld)
 
     for bad in (dict(logp=None), dict(maxpart=None), dict(logpart=None), dict(dlogp=None), dict(dZ=None), dict(dZ=130), dict(ld=99),
-                dict(entropy=None, dentropy=64), dict(dZ=64, ld=101)):
+                dict(entropy=None, dentropy=64), dict(dZ=64, ld=101), dict(dlse=66), dict(maxpart=65)):
         assert grad(rows(), **bad) == SSN_E_INVALID_ARG, bad
     assert grad(rows(ldz=50)) == SSN_E_INVALID_ARG
     assert grad(rows(m=65)) == SSN_E_UNSUPPORTED
@@ -71,7 +74,7 @@ def test_weights_in_4_bits():
     assert L.ssn_q4_margins_workspace(ctypes.byref(b), 0, -1, ctypes.byref(size)) == SSN_E_INVALID_ARG
     assert L.ssn_q4_margins_workspace(ctypes.byref(b), 7, 1, ctypes.byref(size)) == SSN_E_INVALID_ARG
     assert L.ssn_q4_margins_workspace(ctypes.byref(b), binding.SSN_F64, 1, ctypes.byref(size)) == SSN_E_UNSUPPORTED
-    assert L.ssn_q4_margins_workspace(ctypes.byref(b), 0, 1 << 20, ctypes.byref(size)) == SSN_E_UNSUPPORTED
+    assert L.ssn_q4_margins_workspace(ctypes.byref(b), 0, 1 << 19, ctypes.byref(size)) == SSN_E_UNSUPPORTED
     size.value = 5
     assert L.ssn_q4_margins_workspace(ctypes.byref(b), 0, 0, ctypes.byref(size)) == SSN_OK and size.value == 0
     assert L.ssn_q4_margins(None, 0, 1, None, 0, 0, None, 0, None, 0, None) == SSN_E_INVALID_ARG
