@@ -393,11 +393,11 @@ _STAT = {torch.float32: torch.float32, torch.float16: torch.float32, torch.bfloa
 _get_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
-def _ld(t):
-    """Leading dimension of a matrix whose rows are contiguous (the stride of a single row means nothing)."""
-    n, width = t.shape
-    assert width == 1 or t.stride(1) == 1, "rows must be contiguous"
-    return t.stride(0) if n > 1 else width
+def _ld(t, n, width):
+    """Leading dimension of an n x width matrix whose rows are contiguous (the stride of a single row means nothing)."""
+    ld, step = t.stride()
+    assert step == 1 or width == 1, "rows must be contiguous"
+    return ld if n > 1 else width
 
 
 def _elsewhere(t):
@@ -422,7 +422,7 @@ def _rows(Z, labels, k, reference, allowed, dev):
         shape = labels.shape
         assert shape[0] == n and len(shape) <= 2
         at_labels, m = labels.data_ptr(), shape[1] if len(shape) == 2 else 1
-    return ssn_rows(n, C, _DTYPE[Z.dtype], reference, Z.data_ptr(), _ld(Z), at_allowed, ld_allowed, at_labels, m, k,
+    return ssn_rows(n, C, _DTYPE[Z.dtype], reference, Z.data_ptr(), _ld(Z, n, width), at_allowed, ld_allowed, at_labels, m, k,
                     _raw_stream(dev)), n, m
 
 
@@ -487,7 +487,7 @@ def ssn_logprobs_grad(Z, labels, forward, dlogp=None, dlse=None, dentropy=None, 
     st = lib().ssn_logprobs_grad(
         ctypes.byref(d), _data(forward["logp"], stat, n * m, dev) if m else None, _data(forward["maxpart"], stat, n, dev),
         _data(forward["logpart"], stat, n, dev), _data(forward["entropy"], stat, n, dev) if dentropy is not None else None,
-        _data(dlogp, stat, n * m, dev), _data(dlse, stat, n, dev), _data(dentropy, stat, n, dev), dZ.data_ptr(), _ld(dZ))
+        _data(dlogp, stat, n * m, dev), _data(dlse, stat, n, dev), _data(dentropy, stat, n, dev), dZ.data_ptr(), _ld(dZ, *dZ.shape))
     if st != SSN_OK:
         raise SsnError(st, "in ssn_logprobs_grad")
     return dZ
@@ -543,7 +543,7 @@ def ssn_q4_margins(block, X, Z=None):
         Z = torch.empty((n, d.K), dtype=X.dtype, device=X.device)
     assert Z.get_device() == dev and Z.shape == (n, d.K)
     dt, st, L = _DTYPE[X.dtype], _raw_stream(dev), lib()
-    args = (ctypes.byref(d), dt, n, X.data_ptr(), _ld(X), _DTYPE[Z.dtype], Z.data_ptr(), _ld(Z))
+    args = (ctypes.byref(d), dt, n, X.data_ptr(), _ld(X, n, p), _DTYPE[Z.dtype], Z.data_ptr(), _ld(Z, n, d.K))
     status = L.ssn_q4_margins(*args, None, 0, st)
     if status == SSN_E_TOO_LARGE:                   # parts of the features, each with sums of its own
         size = ctypes.c_int64()
