@@ -255,16 +255,16 @@ template <typename A> struct Gather {
         for (int e = 0; e < E; ++e) q.add(x[e]);
     }
     __device__ __forceinline__ Stat<A> done() const { return q; }
-    __device__ __forceinline__ bool beyond() const { return false; }
 };
 // fp32: a margin costs a fused multiply-add, 2^x, an addition, a clamp and a fused multiply-add; the kernel is as much bound
 // by these as by memory.  s and t are kept relative to a power of two: s = sum 2^(c z - M2), t = sum 2^(c z - M2) (c z - M2)
 // with c = log2 e rounded and M2 = c R rounded, both exactly what the multiply-add uses, so that the rounding of M2 is known
 // (r = c R - M2) and taken out at the end.  R follows the largest margin only when it falls more than 13 behind: the terms
-// stay below e^13.  c z overflows for |z| > 2.3e38: rows whose largest margin lies out there are gathered by a Stat instead.
+// stay below e^13.  |r| grows with R, to 0.9 at the edge below: a row whose largest margin is beyond half of that is gathered
+// by a Stat instead, and in any other row a margin below -edge weighs nothing.
 template <> struct Gather<float> {
     float R, M2, s, t, mx;
-    static __device__ __forceinline__ float edge() { return 2e38f; }
+    static __device__ __forceinline__ float edge() { return 1e7f; }
     static __device__ __forceinline__ float c() { return 1.44269504f; }
     __device__ __forceinline__ void init()
     {
@@ -274,6 +274,7 @@ template <> struct Gather<float> {
     }
     template <int E> __device__ __forceinline__ void take(const float (&x)[E], float top)
     {
+#pragma clang fp contract(off)          // M2 - m2 below takes m2 as it is kept, rounded
         mx = fmaxf(mx, top);
         if (__ballot(top - R > 13.0f)) {
             const float to = fmaxf(R, top), m2 = to * c(), d = fmaxf(M2 - m2, -1e4f), f = __builtin_amdgcn_exp2f(d);
@@ -297,8 +298,10 @@ template <> struct Gather<float> {
         else if (mx > R) q.raise(mx);
         return q;
     }
-    __device__ __forceinline__ bool beyond() const { return !(fabsf(mx) < edge()) && mx != minus_inf(0.0f); }
 };
+// whether a row with this largest margin is out of a Gather's reach; fp16 margins never are
+template <typename T> __device__ __forceinline__ bool beyond(float top) { return sizeof(T) == 4 || std::is_same<T, __bf16>::value ? !(fabsf(top) < 5e6f) && top != minus_inf(0.0f) : false; }
+template <typename T> __device__ __forceinline__ bool beyond(double) { return false; }
 
 // One row's answer.  s == 0: no class is left; s != s: the row holds NaN or +inf at an allowed class.
 template <typename A> struct Answer {
@@ -547,15 +550,23 @@ __global__ __launch_bounds__(WAVES *WAVE) void logprobs_wide_kernel(LogprobsArgs
         }
         const A v1 = acc.mx;
         Stat<A> q = acc.done();
-        if (sizeof(T) == 4 || std::is_same<T, __bf16>::value) {
-            if (__ballot(acc.beyond())) {
+        if constexpr (sizeof(T) == 4 || std::is_same<T, __bf16>::value) {
+            A top = wave_max(v1);
+            if (WAVES > 1) {
+                if (lane == 0) sh_kth[wave] = top;
+                __syncthreads();
+                top = wave_max(lane < WAVES ? sh_kth[lane] : minus_inf(A()));
+                __syncthreads();
+            }
+            if (beyond<T>(top)) {
                 q.init();
                 for (int64_t c1 = in.first; c1 < in.end; c1 += STEP) {
-                    Raw raw;
-                    uint32_t word;
+                    Raw far;
+                    uint32_t bits;
                     A x[E];
-                    in.load_any(c1 + lane * E, raw, word);
-                    in.get(c1 + lane * E, raw, word, false, x);
+                    in.load_any(c1 + lane * E, far, bits);
+                    in.get(c1 + lane * E, far, bits, false, x);
+#pragma unroll
                     for (int e = 0; e < E; ++e) {
                         q.raise(take_max(q.M, x[e]));
                         q.add(x[e]);
@@ -817,11 +828,11 @@ template <typename A> struct RowGrad {
     }
     // A vector of them.  16-bit results take one multiply-add for the exponent: with k = c M rounded and r = c M - k, which is
     // exact, p = 2^(c z - k) f with f = 2^(-r - c L), a factor of the row; what is left of p's error, |c (z - M)| 2^-24, is
-    // far below their rounding.  Where c z could overflow, at() does it.
+    // far below their rounding.  Where r is no longer small, at() does it.
     template <typename T, int E> __device__ __forceinline__ void values(A (&x)[E]) const
     {
         if constexpr (sizeof(T) == 2) {
-            if (fabsf(M) < 1e38f) {
+            if (fabsf(M) < 5e6f) {
                 const float c = 1.44269504f, k = M * c, r = fmaf(M, c, -k), f = __builtin_amdgcn_exp2f(-fmaf(L, c, r));
                 if (h == 0.0f) {
                     const float w = -G * f;
@@ -909,7 +920,7 @@ template <typename T, int WAVES> __global__ __launch_bounds__(WAVES *WAVE) void 
                     const int64_t yy = __builtin_amdgcn_readlane(y, from);
                     const A g = at_lane(gy, from);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] += c + e == yy ? g : A(0);
+                    for (int e = 0; e < E; ++e) x[e] += c + e == yy && ((bits >> e) & 1u) ? g : A(0);
                 }
                 if (whole || c + E <= end) {
                     Vec<T>::store(dz + c, pack(x, T()));
@@ -938,9 +949,12 @@ template <typename T, int G> __global__ __launch_bounds__(VEC_BLOCK) void logpro
         T *dz = (T *)a.dZ + row * a.lddz;
         const uint32_t *mask = a.allowed ? a.allowed + row * a.ld_allowed : nullptr;
         for (int c = g; c < a.width; c += G) {
-            A x = w.empty || (mask && !allowed_bit(mask, c)) ? A(0) : w.at((A)z[c]);
-            for (int t = 0; t < a.m; ++t)
-                if (a.labels[row * a.m + t] == c) x += given_weight<A>(a, row * a.m + t, c);
+            A x = A(0);
+            if (!w.empty && (!mask || allowed_bit(mask, c))) {
+                x = w.at((A)z[c]);
+                for (int t = 0; t < a.m; ++t)
+                    if (a.labels[row * a.m + t] == c) x += given_weight<A>(a, row * a.m + t, c);
+            }
             dz[c] = (T)x;
         }
     }

@@ -209,6 +209,43 @@ def test_special_values(dtype, C):
     check(Zd, h, y, min(C, 17), True, np.concatenate([mask, rng.random((12, 1)) < 0.5], 1))
 
 
+@pytest.mark.parametrize("C", [9, 700, 5000, 40000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f64"])
+def test_margins_far_from_zero(dtype, C):
+    """Rows around values whose product with log2 e is rounded by more than one, up to the edge of the type; rows filled with
+    -1e9 or -1e30 but for a few classes, or for one half; neighbours two steps apart out there."""
+    dt, rng = DTYPES[dtype], np.random.default_rng(C)
+    sizes = [4e6, 6e6, 1.1e7, 1e8, 3e9, 1e12, 1e20, 1e30, 3e37]
+    h = np.zeros((4 * len(sizes) + 4, C))
+    for i, v in enumerate(sizes):
+        h[4 * i], h[4 * i + 1] = v, -v
+        h[4 * i + 2], h[4 * i + 3] = v * (1 + rng.integers(-2, 1, C) * 2.0 ** -7), -v * (1 + rng.integers(0, 3, C) * 2.0 ** -7)
+    h[-4:] = [[-1e9], [-1e30], [-1e9], [-9.9e6]]
+    h[-4, 3::61], h[-3, C // 2:] = rng.standard_normal(len(h[0, 3::61])), rng.standard_normal(C - C // 2)
+    h[-2, -1] = -1e9 + 128
+    h[-1, C // 2:] = -1.0001e7
+    h = torch.from_numpy(h).to(dt).double().numpy()
+    y = np.stack([np.full(len(h), C - 1), rng.integers(0, C, len(h))], 1)
+    for reference in (False, True):
+        check(torch.from_numpy(h).to(dt).cuda(), h, y, 5, reference, None)
+
+
+def test_nothing_at_classes_that_are_not_allowed():
+    """Also where the row has no distribution, or a given class is not allowed or none."""
+    for C in (40, 3000):
+        Z = torch.randn(4, C, device="cuda")
+        Z[1, 7], Z[2, 8] = float("nan"), float("inf")
+        mask = np.ones((4, C), dtype=bool)
+        mask[:, 20:30] = False
+        lab = torch.tensor([[25, 1], [25, 1], [21, 22], [25, C]], dtype=torch.int32, device="cuda")
+        out = ssn_logprobs(Z, lab, allowed=bits(mask))
+        dZ = ssn_logprobs_grad(Z, lab, out, dlogp=torch.ones(4, 2, device="cuda"), allowed=bits(mask))
+        assert bool((dZ[:, 20:30] == 0).all())
+        keep = torch.ones(C, dtype=torch.bool)
+        keep[20:30] = False
+        assert bool(torch.isnan(dZ[1:, keep]).all()) and bool(torch.isfinite(dZ[0]).all())
+
+
 def test_given_classes_of_every_kind():
     """The same class given several times, padding, an index that is no class: values and gradients."""
     rng = np.random.default_rng(3)
