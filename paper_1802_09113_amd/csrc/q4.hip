@@ -582,7 +582,7 @@ __global__ __launch_bounds__(VEC_BLOCK) void q4_quantize_kernel(const T *W, int6
 //   128 rows x 256 classes 64 us, 32 x 128 115 us; 128 rows, 4096 x 8192: 32 x 128 21 us, 128 x 256 64 us).
 namespace {
 enum Q4Form : int {
-    Q4_ROWS4, Q4_ROWS4_WIDE, Q4_ROWS8, Q4_ROWS8_WIDE, Q4_ROWS16, Q4_ROWS16_WIDE,       // stream kernel
+    Q4_ROWS4, Q4_ROWS4_WIDE, Q4_ROWS8, Q4_ROWS8_SPLIT, Q4_ROWS8_WIDE, Q4_ROWS16, Q4_ROWS16_WIDE,       // stream kernel
     Q4_TILE16, Q4_TILE16_HALF, Q4_TILE32, Q4_TILE64, Q4_TILE64_WIDE, Q4_TILE128         // tile kernel: rows of a workgroup
 };
 int64_t groups_of(int64_t n, int64_t K, int rows, int classes) { return (n + rows - 1) / rows * ((K + classes - 1) / classes); }
@@ -597,7 +597,8 @@ void q4_plan(int num_cus, Q4Args *a)
         a->form = tiles >= (split ? 7 : 10) * num_cus / 2 ? Q4_ROWS4_WIDE : Q4_ROWS4;
         groups = a->form == Q4_ROWS4 ? tiles : tiles / 4;
     } else if (n <= 8) {
-        a->form = tiles >= (split ? 8 : 10) * num_cus / 2 ? Q4_ROWS8_WIDE : Q4_ROWS8;
+        // splitting fp32 rows is worth four tiles sooner (5 rows, 5003 x 10007: 13.5 us, two tiles 15.0 us)
+        a->form = tiles >= (split ? 6 : 5) * num_cus ? Q4_ROWS8_WIDE : split && tiles >= 2 * num_cus ? Q4_ROWS8_SPLIT : Q4_ROWS8;
         groups = a->form == Q4_ROWS8 ? tiles / 2 + 1 : tiles / 4;
     } else if (a->p < BLOCK || (n <= 16 && (!split || tiles < 4 * num_cus))) {
         a->form = tiles >= (split ? 2 : 3) * num_cus ? Q4_ROWS16_WIDE : Q4_ROWS16;
@@ -648,6 +649,9 @@ template <typename T, int GROUP> static void q4_launch(const Q4Args &a, hipStrea
     case Q4_ROWS4: stream(one, one, eight, two); return;
     case Q4_ROWS4_WIDE: stream(one, four, wide, one); return;
     case Q4_ROWS8: stream(two, two, eight, one); return;
+    case Q4_ROWS8_SPLIT:
+        if constexpr (SPLIT) stream(two, four, eight, one);
+        return;
     case Q4_ROWS8_WIDE: stream(two, four, four, one); return;
     case Q4_ROWS16: stream(four, two, eight, one); return;
     case Q4_ROWS16_WIDE: stream(four, four, eight, one); return;

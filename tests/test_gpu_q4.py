@@ -145,7 +145,7 @@ def test_margins(dtype, group, n, p, K):
 # as many classes as it takes for each form to serve (256 compute units); odd numbers of rows, features and classes
 @pytest.mark.parametrize("dtype,group,n,p,K", [
     ("bf16", 32, 1, 300, 20500), ("f16", 64, 3, 1025, 24001), ("f32", 32, 2, 300, 14500), ("bf16", 128, 6, 300, 20500),
-    ("f32", 64, 7, 300, 16500), ("f16", 32, 12, 300, 12500), ("f32", 128, 11, 300, 8300), ("f32", 32, 13, 300, 16500),
+    ("f32", 64, 7, 300, 16500), ("f32", 32, 8, 300, 8300), ("f32", 64, 5, 300, 24700), ("f16", 32, 12, 300, 12500), ("f32", 128, 11, 300, 8300), ("f32", 32, 13, 300, 16500),
     ("f32", 32, 30, 140, 33001), ("bf16", 32, 100, 300, 5200), ("f16", 128, 40, 300, 20501), ("bf16", 64, 200, 300, 11001),
     ("f16", 32, 130, 300, 20501), ("bf16", 128, 257, 128, 20480), ("bf16", 32, 150, 127, 2000), ("f32", 32, 40, 100, 700)])
 def test_margins_of_many_classes(dtype, group, n, p, K):
