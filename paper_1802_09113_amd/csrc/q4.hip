@@ -146,15 +146,16 @@ template <typename Z> __device__ __forceinline__ void store_margins(Z *z, int64_
     }
 }
 
-// `waves` waves share a stretch of the blocks of OT tiles and add their sums in a fixed order.  Row r of a group of 16 stands
-// at place 4 (r % 4) + r / 4 of the matrix operand: its sums are then in register r / 4 of lane group r % 4, and up to
-// four rows need one register of the four (USED = 1).  Places without a row hold the last row again; their sums are not
-// stored.
+// the scales of a class in a block, in one load
 template <int GROUPS> struct ScaleWord;
 template <> struct ScaleWord<1> { typedef uint16_t type; };
 template <> struct ScaleWord<2> { typedef uint32_t type; };
 template <> struct ScaleWord<4> { typedef uint64_t type; };
 
+// WAVES waves share a stretch of the blocks of OT tiles and add their sums in a fixed order.  Row r of a group of 16 stands
+// at place 4 (r % 4) + r / 4 of the matrix operand: its sums are then in register r / 4 of lane group r % 4, and up to
+// four rows need one register of the four (USED = 1).  Places without a row hold the last row again; their sums are not
+// stored.
 template <typename T, int GROUP, int USED, int OT, int WAVES, int DEPTH>
 __global__ __launch_bounds__(WAVES *WAVE) void q4_stream_kernel(Q4Args a)
 {
