@@ -6,7 +6,8 @@
 // and log s in [0, log C] is kept apart from M, so that log p_y carries no rounding of a large log-sum-exp.  One pass over
 // the row: every lane keeps (M, s, t) of what it has seen and rescales s and t when its M grows; pairs are joined the same
 // way across lanes, waves and workgroups.  s is NaN exactly when a margin is NaN or +inf, and 0 exactly when no class is
-// left (the largest margin contributes e^0 = 1).  All of it in fp32 for fp32, fp16 and bf16 margins, in fp64 for fp64.
+// left (the largest margin contributes e^0 = 1).  A lane may let its M lag a little behind (Gather), and takes back what its t
+// then holds too much before it is joined.  All of it in fp32 for fp32, fp16 and bf16 margins, in fp64 for fp64.
 //
 // What bounds it: memory on many long rows (8192 x 65536 bf16, one label: 179 us, 6.0 TB/s; the vector units are 60 % busy
 // with some nine instructions a margin), the vector units where a row is one workgroup's and alternatives are asked for, and
@@ -259,11 +260,15 @@ template <typename A> struct Gather {
 // fp32: a margin costs a fused multiply-add, 2^x, an addition, a clamp and a fused multiply-add; the kernel is as much bound
 // by these as by memory.  s and t are kept relative to a power of two: s = sum 2^(c z - M2), t = sum 2^(c z - M2) (c z - M2)
 // with c = log2 e rounded and M2 = c R rounded, both exactly what the multiply-add uses, so that the rounding of M2 is known
-// (r = c R - M2) and taken out at the end.  R follows the largest margin only when it falls more than 13 behind: the terms
-// stay below e^13.  |r| grows with R, to 0.9 at the edge below: a row whose largest margin is beyond half of that is gathered
-// by a Stat instead, and in any other row a margin below -edge weighs nothing.
+// (r = c R - M2) and taken out at the end.  R follows the largest margin when it falls more than LAG behind.  What t holds too
+// much and done() takes back is at most LAG s, and the heaviest terms are rescaled by no more than e^-LAG: a wider lag saves
+// rescalings and costs a confident row its last bits (a best class behind margins 3 to 13 below it in its lane, 256 x 65536:
+// entropy off by 8 u with a lag of 13, u = 2^-24, root mean square, by 3 u with two or one; 8192 x 65536 bf16 179, 183 and
+// 187 us).  |r| grows with R, to 0.9 at the edge below: a row whose largest margin is beyond half of that is gathered by a
+// Stat instead, and in any other row a margin below -edge weighs nothing.
 template <> struct Gather<float> {
     float R, M2, s, t, mx;
+    static constexpr float LAG = 2.0f;
     static __device__ __forceinline__ float edge() { return 1e7f; }
     static __device__ __forceinline__ float c() { return 1.44269504f; }
     __device__ __forceinline__ void init()
@@ -276,7 +281,7 @@ template <> struct Gather<float> {
     {
 #pragma clang fp contract(off)          // M2 - m2 below takes m2 as it is kept, rounded
         mx = fmaxf(mx, top);
-        if (__ballot(top - R > 13.0f)) {
+        if (__ballot(top - R > LAG)) {
             const float to = fmaxf(R, top), m2 = to * c(), d = fmaxf(M2 - m2, -1e4f), f = __builtin_amdgcn_exp2f(d);
             t = (t + s * d) * f;
             s *= f;
