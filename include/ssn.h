@@ -341,6 +341,7 @@ typedef struct {
  *   - a row without a class of more than -inf: M = -inf, L = 0, entropy 0, every log probability -inf.
  *   - a row with NaN or +inf at an allowed class has no distribution: NaN in all its values, classes -1.
  *   - a given class < 0 is padding: 0.  A given class >= C: NaN.
+ *   - where there is a distribution: L >= 0, entropy >= 0, no log probability above 0, exactly.
  * logp may be NULL if m is 0, top_ids and top_logp if k is 0.  workspace [dev], 8-byte aligned, of at least the size that
  * ssn_logprobs_workspace stores in *bytes for the same n, C, dtype, reference and k (often 0; then it may be NULL); only
  * for the duration of the call's kernels.  Returns SSN_OK, SSN_E_INVALID_ARG, SSN_E_UNSUPPORTED (n, C, m or k too large),

@@ -308,13 +308,23 @@ template <> struct Gather<float> {
 template <typename T> __device__ __forceinline__ bool beyond(float top) { return sizeof(T) == 4 || std::is_same<T, __bf16>::value ? !(fabsf(top) < 5e6f) && top != minus_inf(0.0f) : false; }
 template <typename T> __device__ __forceinline__ bool beyond(double) { return false; }
 
-// One row's answer.  s == 0: no class is left; s != s: the row holds NaN or +inf at an allowed class.
+// One row's answer.  s == 0: no class is left; s != s: the row holds NaN or +inf at an allowed class.  Any other row has s >= 1,
+// but where a Gather's reference is a power of two its largest margin's term is two rounded factors and may miss 1 by their
+// error: no log probability is above zero, and no entropy below.
 template <typename A> struct Answer {
     A M, L, s, t;
-    __device__ __forceinline__ Answer(const Stat<A> &q) : M(q.M), s(q.s), t(q.t) { L = s == A(0) ? A(0) : log_sum(s); }
+    __device__ __forceinline__ Answer(const Stat<A> &q) : M(q.M), s(q.s), t(q.t)
+    {
+        if (s > A(0) && s < A(1)) s = A(1);
+        L = s == A(0) ? A(0) : log_sum(s);
+    }
     __device__ __forceinline__ A maxpart() const { return s == A(0) ? minus_inf(A()) : s == s ? M : s; }
     __device__ __forceinline__ A logpart() const { return L; }
-    __device__ __forceinline__ A entropy() const { return s == A(0) ? A(0) : L - t / s; }
+    __device__ __forceinline__ A entropy() const
+    {
+        const A h = s == A(0) ? A(0) : L - t / s;
+        return h < A(0) ? A(0) : h;                                    // NaN stays
+    }
     __device__ __forceinline__ A logp(A z) const
     {
         if (!(s == s)) return s;

@@ -74,3 +74,23 @@ def test_a_best_class_behind_margins_of_the_same_lane(dtype, n, C):
     eL, eH = ((square / seen).sqrt() / U).tolist()
     print(f"[case] n={n} C={C} {dtype}: L {eL:.2f} u, H {eH:.2f} u", flush=True)
     assert eL <= 24 ** 0.5 and eH <= 48 ** 0.5
+
+
+@pytest.mark.parametrize("n,C", [(4096, 300), (4096, 700), (3000, 5000), (600, 9001), (100, 40000), (3, 131077)])
+@pytest.mark.parametrize("dtype", list(DTYPES) + ["f64"])
+def test_signs(dtype, n, C):
+    """logpart >= 0, entropy >= 0 and no log probability above zero, exactly: rows of one class, or of a class that has all the
+    weight, at every size of its margin."""
+    dt = DTYPES.get(dtype, torch.float64)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(C)
+    for scale in (1.0, 30.0, 3000.0):
+        best = torch.randint(C, (n, 1), generator=g, device="cuda")
+        Z = scale * torch.randn(n, C, generator=g, device="cuda") - 40 * scale
+        Z = Z.scatter_(1, best, scale * torch.randn(n, 1, generator=g, device="cuda"))
+        Z[::3] = torch.where(torch.arange(C, device="cuda") == best[::3], Z[::3], -float("inf"))
+        out = ssn_logprobs(Z.to(dt), best.to(torch.int32), k=2)
+        print(f"[case] n={n} C={C} {dtype} scale={scale} lowest logpart {float(out['logpart'].min()):.3g}", flush=True)
+        assert bool((out["logpart"] >= 0).all()) and bool((out["entropy"] >= 0).all())
+        assert bool((out["logp"] <= 0).all()) and bool((out["top_logp"] <= 0).all())
+        assert bool((out["top_ids"][:, :1] == best).all())
