@@ -386,8 +386,11 @@ int ssn_q4_quantize(const ssn_q4 *block, int32_t dtype, const void *W, int64_t s
 
 /* Margins of rows of features with such a block: Z = X W, z_ic = sum_j x_ij w_jc.  X [dev] n rows of p elements, leading
  * dimension ldx >= p, SSN_F32, SSN_F16 or SSN_BF16; Z [dev] n rows of K elements, leading dimension ldz >= K, of type
- * zdtype: X's or SSN_F32; both aligned to an element.  Products are exact, sums in fp32, rounded once to Z's type; the
- * order of the sums depends on the sizes only, also on n.  Z must not overlap X.  n = 0: nothing is done.  workspace [dev],
+ * zdtype: X's or SSN_F32; both aligned to an element.  Sums are formed in fp32 and rounded once to Z's type: the products of
+ * code numbers and features, which are exact, over a group, then the groups' sums times their scales.  The order of the sums
+ * depends on the sizes only, also on n.  The features may have any finite size; at the lower end, bits of a float feature
+ * below 2^-133 are not seen (features of 2^-110 and more have none), and with float and bfloat16 features a sum of groups loses
+ * its bits below 2^-139.  Z must not overlap X.  n = 0: nothing is done.  workspace [dev],
  * 4-byte aligned, of at least the size that ssn_q4_margins_workspace stores in *bytes for the same sizes (often 0; then it
  * may be NULL).  Returns SSN_OK, SSN_E_INVALID_ARG, SSN_E_UNSUPPORTED (n of 2^19 or more, SSN_F64), SSN_E_TOO_LARGE
  * (workspace too small) or SSN_E_HIP. */

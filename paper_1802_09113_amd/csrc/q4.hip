@@ -4,8 +4,12 @@
 // Why these magnitudes: gfx950 converts two such codes to bfloat16 or half precision in one instruction, exactly, and
 // both types feed the matrix cores.  A product of a code's number with a bfloat16 / half value is exact in fp32, so a
 // group's sum over its features is an fp32 sum of exact products; the scale is applied to that sum in fp32.  Rows in
-// fp32 are split into three bfloat16 parts of eight significant bits each, x = x0 + x1 + x2 exactly, and take three
-// products.
+// fp32 are split into three bfloat16 parts of eight significant bits each, x = x0 + x1 + x2, and take three products.
+// That is exact down to the last bit that a bfloat16 number has, 2^-133.
+//
+// A group's sum is formed before its scale, so it may be 768 times the largest feature where the margin is small.  Bfloat16
+// codes are therefore converted to 2^-10 of their numbers, which the instruction does for nothing, and a margin's sum carries
+// that factor until it is stored: no finite features overflow, and what a sum loses are its bits below 2^-139.
 //
 // Layout: tiles of 16 classes, blocks of 128 features; a block of a tile is 1 KB, 16 bytes for each lane (g, o) =
 // (lane / 16, lane % 16): word j of them holds features 128 b + 32 j + 8 g + 0..7 of class 16 t + o, which is lane (g, o)'s
@@ -40,11 +44,12 @@ __device__ __forceinline__ float bf16_value(uint16_t b) { return __uint_as_float
 template <typename T> struct Rows;
 template <> struct Rows<__bf16> {
     static constexpr int PIECES = 1;
+    static constexpr float UNIT = 0.0009765625f;                       // what the codes are multiplied with, 2^-10
     typedef B8 Op;
     static __device__ __forceinline__ Op codes(uint32_t w)
     {
-        const B2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1);
-        const B2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3);
+        const B2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, UNIT, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, UNIT, 1);
+        const B2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, UNIT, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, UNIT, 3);
         return Op{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     }
     static __device__ __forceinline__ void operand(const Raw (&r)[1], Op (&o)[1]) { o[0] = __builtin_bit_cast(Op, r[0]); }
@@ -53,6 +58,7 @@ template <> struct Rows<__bf16> {
 };
 template <> struct Rows<_Float16> {
     static constexpr int PIECES = 1;
+    static constexpr float UNIT = 1.0f;                                // 768 times the largest half is no large float
     typedef H8 Op;
     static __device__ __forceinline__ Op codes(uint32_t w)
     {
@@ -66,6 +72,7 @@ template <> struct Rows<_Float16> {
 };
 template <> struct Rows<float> {
     static constexpr int PIECES = 3;
+    static constexpr float UNIT = Rows<__bf16>::UNIT;
     typedef B8 Op;
     static __device__ __forceinline__ Op codes(uint32_t w) { return Rows<__bf16>::codes(w); }
     // the three parts of two features, a word of two bfloat16 numbers each
@@ -293,7 +300,7 @@ __global__ __launch_bounds__(WAVES *WAVE) void q4_stream_kernel(Q4Args a)
 #pragma unroll
         for (int i = 1; i < WAVES; ++i) v += sums[i][rr][cc];
         if (a.parts > 1) a.ws[((int64_t)blockIdx.y * a.n + r) * a.K + c] = v;
-        else store_margin(a.Z, a.zdtype, r * a.ldz + c, v);
+        else store_margin(a.Z, a.zdtype, r * a.ldz + c, v * (1.0f / Rows<T>::UNIT));
     }
 }
 
@@ -483,7 +490,8 @@ __global__ __launch_bounds__(WM *WN *WK *WAVE) void q4_tile_kernel(Q4Args a)
             const int rr = h * 8 + (lane >> 3);
             const int64_t r = r0 + wm * 16 * RT + rt * 16 + rr;
             const F4 lo = *(const F4 *)(out + rr * LINE + (lane & 7) * 8), hi = *(const F4 *)(out + rr * LINE + (lane & 7) * 8 + 4);
-            const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            const float u = a.parts > 1 ? 1.0f : 1.0f / Rows<T>::UNIT;
+            const float v[8] = {lo[0] * u, lo[1] * u, lo[2] * u, lo[3] * u, hi[0] * u, hi[1] * u, hi[2] * u, hi[3] * u};
             if (r >= a.n || c >= a.K) continue;
             if (a.parts > 1) store_margins((float *)a.ws + ((int64_t)blockIdx.y * a.n + r) * a.K + c, a.K - c, v);
             else if (a.zdtype == SSN_F32) store_margins((float *)a.Z + r * a.ldz + c, a.K - c, v);
@@ -493,14 +501,15 @@ __global__ __launch_bounds__(WM *WN *WK *WAVE) void q4_tile_kernel(Q4Args a)
     }
 }
 
-// the parts' sums in order
+// the parts' sums in order; what the codes were multiplied with is taken out of the margin
 __global__ __launch_bounds__(VEC_BLOCK) void q4_join_kernel(Q4Args a)
 {
+    const float u = a.dtype == SSN_F16 ? 1.0f / Rows<_Float16>::UNIT : 1.0f / Rows<__bf16>::UNIT;
     for (int64_t r = blockIdx.y; r < a.n; r += gridDim.y)
         for (int64_t c = (int64_t)blockIdx.x * VEC_BLOCK + threadIdx.x; c < a.K; c += (int64_t)gridDim.x * VEC_BLOCK) {
             float v = 0.0f;
             for (int i = 0; i < a.parts; ++i) v += a.ws[((int64_t)i * a.n + r) * a.K + c];
-            store_margin(a.Z, a.zdtype, r * a.ldz + c, v);
+            store_margin(a.Z, a.zdtype, r * a.ldz + c, v * u);
         }
 }
 
