@@ -386,11 +386,18 @@ class Context:
 
 # ---- a softmax layer over many classes -----------------------------------------------------------------------------
 # The smallest of these calls are a kernel of a few microseconds: what the binding does around them is kept to plain
-# attribute reads (torch's own accessors of the current device and stream, one library call where no workspace is needed).
+# attribute reads and one library call where no workspace is needed.  They take and return plain data: torch records no graph
+# of them, and a gradient is asked for with ssn_logprobs_grad.
 
 _DTYPE = {torch.float32: SSN_F32, torch.float64: SSN_F64, torch.float16: SSN_F16, torch.bfloat16: SSN_BF16}
 _STAT = {torch.float32: torch.float32, torch.float16: torch.float32, torch.bfloat16: torch.float32, torch.float64: torch.float64}
-_get_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _raw_stream(dev):
+    """The current stream of a device as a hipStream_t: from torch's table of handles where this torch has that accessor
+    (0.1 us), else from a stream object (1.1 us)."""
+    handle = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return handle(dev) if handle else torch.cuda.current_stream(dev).cuda_stream
 
 
 def _ld(t, n, width):
@@ -403,7 +410,7 @@ def _ld(t, n, width):
 def _elsewhere(t):
     """Whether t lives on another device than the current one (kernels go to its device's current stream)."""
     assert t.is_cuda
-    return t.get_device() != _get_device()
+    return t.get_device() != torch.cuda.current_device()
 
 
 def _rows(Z, labels, k, reference, allowed, dev):
@@ -441,7 +448,8 @@ def ssn_logprobs(Z, labels=None, k=0, reference=False, allowed=None, out=None):
     class C - 1 has margin zero.  labels: int32, (n,) or (n, m), negative = padding.  allowed: int32 words of bits, (n,
     ceil(C / 32)) or one row of words for all.  Returns a dict of logp (shaped like labels), maxpart, logpart, entropy
     and, with k > 0, top_ids and top_logp; `out` may bring any of them (missing or None: entropy, maxpart and logpart are
-    then not computed, the others allocated)."""
+    then not computed, the others allocated).  Nothing of it requires a gradient, whatever Z does: ssn_logprobs_grad is the
+    backward pass, to be called by itself or by a torch.autograd.Function of the caller's."""
     if _elsewhere(Z):
         with torch.cuda.device(Z.device):
             return ssn_logprobs(Z, labels, k, reference, allowed, out)
