@@ -2,13 +2,20 @@
 
 Next to the library the build leaves kernel_resources.json: registers and scratch bytes per lane of every
 kernel, from the compiler's own resource remarks.  A kernel that uses scratch memory at all pays ~14 us per
-launch on MI355X, so the test suite checks that none of this library's kernels does."""
+launch on MI355X, so the test suite checks that none of this library's kernels does.
+
+The compiler's code goes through its assembler as text.  The compiler of ROCm 7.2 keeps a wave-uniform fp64 constant such as -inf
+in a pair of scalar registers and fills them with one 64-bit instruction, whose encoding holds half of the number: written
+straight into an object file such code is silently wrong, as text the assembler refuses it and the build fails.
+"""
 import glob
 import json
 import os
 import re
+import shutil
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -44,11 +51,17 @@ def _resources(remarks):
 
 
 def build(verbose=False):
+    with tempfile.TemporaryDirectory() as temps:             # the assembly's
+        return _build(verbose, temps)
+
+
+def _build(verbose, temps):
     procs = []
     for src in SRCS:                      # every source at once: one long file dominates the build
-        obj = src[:-4] + ".o"
+        name = os.path.basename(src)[:-4]
+        obj = os.path.join(temps, name + ".o")
         cmd = (["hipcc", "-c"] + [f for f in FLAGS if f != "-shared"]
-               + ["-Rpass-analysis=kernel-resource-usage", "-o", obj, src])
+               + ["-Rpass-analysis=kernel-resource-usage", "-save-temps=obj", "-o", obj, src])
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, obj, cmd, subprocess.Popen(cmd, stderr=subprocess.PIPE, text=True)))
@@ -59,7 +72,7 @@ def build(verbose=False):
             sys.stderr.write(err)
             raise subprocess.CalledProcessError(proc.returncode, cmd)
         resources[os.path.basename(src)] = _resources(err)
-        objs.append(obj)
+        objs.append(shutil.copy(obj, src[:-4] + ".o"))
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs
     if verbose:
         print(" ".join(cmd), flush=True)

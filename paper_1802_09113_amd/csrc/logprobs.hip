@@ -109,7 +109,8 @@ __device__ __forceinline__ double lowest(double) { return -__DBL_MAX__; }
 __device__ __forceinline__ float minus_inf(float) { return -__builtin_inff(); }
 __device__ __forceinline__ double minus_inf(double) { return -__builtin_inf(); }
 // -inf that the compiler does not know: it would keep a wave's constant of this value in a pair of scalar registers, and
-// writes it there with one instruction that holds only half of the number
+// writes it there with one instruction that holds only half of the number.  Where minus_inf(double) stands below the compiler
+// does not do that; the build goes through the assembler's text, which refuses it.
 __device__ __forceinline__ float hidden_minus_inf(float) { return minus_inf(0.0f); }
 __device__ __forceinline__ double hidden_minus_inf(double)
 {
