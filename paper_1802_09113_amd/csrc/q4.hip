@@ -635,20 +635,40 @@ void q4_plan(int num_cus, Q4Args *a)
 
 int64_t q4_workspace(const Q4Args &a) { return a.parts > 1 ? (int64_t)a.parts * a.n * a.K * 4 : 0; }
 
+// Workgroups of one launch: their threads have to fit 32 bits.  More classes take a launch for each stretch of them.
+static constexpr int64_t MAX_GRID = 1 << 20;
+
+// f(arguments, tiles) for stretches of at most `most` tiles of classes.  More than one only where the rows are not split.
+template <typename F> static void each_stretch(const Q4Args &a, int64_t most, F f)
+{
+    const int64_t tiles = (a.K + TILE - 1) / TILE, blocks = (a.p + BLOCK - 1) / BLOCK;
+    for (int64_t t = 0; t < tiles; t += most) {
+        Q4Args b = a;
+        b.packed += t * blocks * (WAVE * sizeof(Raw));
+        b.scales += t * blocks * (TILE * BLOCK / a.group);
+        b.Z = (char *)a.Z + t * TILE * (a.zdtype == SSN_F32 ? 4 : 2);
+        b.K = a.K - t * TILE < most * TILE ? a.K - t * TILE : most * TILE;
+        f(b, (b.K + TILE - 1) / TILE);
+    }
+}
+
 template <typename T, int GROUP> static void q4_launch(const Q4Args &a, hipStream_t st)
 {
     constexpr bool SPLIT = sizeof(T) == 4;
-    const int64_t tiles = (a.K + TILE - 1) / TILE;
     auto stream = [&](auto used, auto ot, auto waves, auto depth) {
         constexpr int USED = decltype(used)::value, OT = decltype(ot)::value, WAVES = decltype(waves)::value;
-        const dim3 grid((unsigned)((tiles + OT - 1) / OT), (unsigned)a.parts, (unsigned)((a.n + 15) / 16));
-        hipLaunchKernelGGL((q4_stream_kernel<T, GROUP, USED, OT, WAVES, decltype(depth)::value>), grid, dim3(WAVES * WAVE), 0, st, a);
+        each_stretch(a, MAX_GRID * OT, [&](const Q4Args &b, int64_t tiles) {
+            const dim3 grid((unsigned)((tiles + OT - 1) / OT), (unsigned)a.parts, (unsigned)((a.n + 15) / 16));
+            hipLaunchKernelGGL((q4_stream_kernel<T, GROUP, USED, OT, WAVES, decltype(depth)::value>), grid, dim3(WAVES * WAVE), 0, st, b);
+        });
     };
     auto tile = [&](auto rt, auto wm, auto wn, auto wk) {
         constexpr int RT = decltype(rt)::value, WM = decltype(wm)::value, WN = decltype(wn)::value, WK = decltype(wk)::value;
-        const int64_t groups = (a.n + 16 * RT * WM - 1) / (16 * RT * WM) * ((tiles + 4 * WN - 1) / (4 * WN));
-        const dim3 grid((unsigned)groups, (unsigned)a.parts);
-        hipLaunchKernelGGL((q4_tile_kernel<T, GROUP, RT, WM, WN, WK>), grid, dim3(WM * WN * WK * WAVE), 0, st, a);
+        const int64_t row_groups = (a.n + 16 * RT * WM - 1) / (16 * RT * WM);              // at most 2^15
+        each_stretch(a, MAX_GRID / row_groups * (4 * WN), [&](const Q4Args &b, int64_t tiles) {
+            const dim3 grid((unsigned)(row_groups * ((tiles + 4 * WN - 1) / (4 * WN))), (unsigned)a.parts);
+            hipLaunchKernelGGL((q4_tile_kernel<T, GROUP, RT, WM, WN, WK>), grid, dim3(WM * WN * WK * WAVE), 0, st, b);
+        });
     };
     std::integral_constant<int, 1> one;
     std::integral_constant<int, 2> two;
@@ -701,11 +721,15 @@ hipError_t launch_q4_margins(Q4Args &a, void *workspace, hipStream_t st)
 hipError_t launch_q4_quantize(int dtype, int64_t p, int64_t K, const void *W, int64_t sj, int64_t sc, int group, uint8_t *packed,
                               uint16_t *scales, hipStream_t st)
 {
-    const int64_t blocks = (p + BLOCK - 1) / BLOCK, ct = (K + QUANT_TILES * TILE - 1) / (QUANT_TILES * TILE);
-    const dim3 grid((unsigned)ct, (unsigned)(blocks < 65535 ? blocks : 65535));
+    const int64_t blocks = (p + BLOCK - 1) / BLOCK, most = MAX_GRID * QUANT_TILES * TILE;
     auto go = [&](auto tag) {
         typedef decltype(tag) T;
-        hipLaunchKernelGGL(q4_quantize_kernel<T>, grid, dim3(VEC_BLOCK), 0, st, (const T *)W, sj, sc, p, K, group, packed, scales);
+        for (int64_t c = 0; c < K; c += most) {
+            const int64_t t = c / TILE, left = K - c < most ? K - c : most;
+            const dim3 grid((unsigned)((left + QUANT_TILES * TILE - 1) / (QUANT_TILES * TILE)), (unsigned)(blocks < 65535 ? blocks : 65535));
+            hipLaunchKernelGGL(q4_quantize_kernel<T>, grid, dim3(VEC_BLOCK), 0, st, (const T *)W + c * sc, sj, sc, p, left, group,
+                               packed + t * blocks * (WAVE * sizeof(Raw)), scales + t * blocks * (TILE * BLOCK / group));
+        }
     };
     if (dtype == SSN_F32) go(float());
     else if (dtype == SSN_F64) go(double());
