@@ -1015,11 +1015,14 @@ void logprobs_plan(int dtype, int64_t n, int64_t C, int64_t width, int k, int nu
     if (C <= WAVE * NARROW_PER_LANE) return;
     const int64_t steps = (width + step - 1) / step;                   // loads of a whole wave that the row takes
     const int most = dtype == SSN_F64 ? 8 : 16, ahead = dtype == SSN_F64 ? 2 : 4;
-    // Rows enough to fill the chip: as few waves per row as keep its loads in flight, since joining them costs (3000 rows of
-    // 5000 fp32: one wave 21 us, four 24 us, eight 35 us; 8192 of 65536 bf16: four 187 us, eight 179 us, sixteen 238 us).
-    // Fewer rows than compute units: all the waves a workgroup may have, and several workgroups per row where each wave
-    // still has loads for one round of AHEAD (one row of 131072 fp32: one workgroup 18 us, eight 11 us; of 32000: one 9.2 us,
-    // two 10.3 us, since the join is a launch of its own).
+    // Figures in us on 256 compute units.  Rows enough to fill the chip: as few waves per row as keep its loads in flight, since
+    // joining them costs (bf16, one / four / eight waves: 3000 rows of 4096 9.4 / 11.9 / 17.7, of 12288 17.7 / 19.3 / 22.0;
+    // 600 of 12288 10.8 / 7.3 / 7.5; 3000 of 32768 42.9 / 41.5 / 41.8, of 65536 77.5 / 76.7 / 72.6; sixteen 103).  Rows of
+    // eight loads or less are one wave's however few (100 of 2048 4.1 / 4.1, of 4096 5.1 / 4.3, less than the call costs the host).
+    // Fewer rows than compute units: all the waves a workgroup may have (100 of 8192 bf16: eight 4.5, sixteen 5.2; of 65536
+    // 9.1, 8.7), and several workgroups per row where each wave still has loads for one round of AHEAD (one row of 131072
+    // fp32, five alternatives: one workgroup 19.4, eight 10.7; of 40960 10.8, four 10.4; of 32000 9.4, two 10.3, since the
+    // join is a launch of its own).
     if (steps <= 8 || (steps <= 24 && n >= 8 * num_cus)) {
         a->waves = 1;
     } else if (n >= 2 * num_cus) {
@@ -1097,9 +1100,11 @@ hipError_t launch_logprobs_grad(int dtype, const LogprobsArgs &a, hipStream_t st
             });
             return;
         }
-        // A short row is one wave's.  A workgroup takes two rounds of loads, the second of which is on its way while the first
-        // is worked on (8192 x 65536 bf16: one round 457 us, two 353 us, four 391 us), or one where two would leave compute
-        // units without work (4 x 32000 fp32: 5.5 and 6.3 us).
+        // A short row is one wave's (bf16, one wave / four: 20000 rows of 2048 27 / 49 us, 1000 of 3000 5.6 / 5.5 us).  A
+        // workgroup takes two rounds of loads, the second of which is on its way while the first is worked on (8192 x 65536
+        // bf16: one round 470 us, two 357 us, four 400 us), or one where two would leave compute units without work
+        // (4 x 32000: 3.4 and 4.4 us).  Rows of up to 256 classes share waves (20000 fp32 rows of 100: 9.9 us, a wave each
+        // 12.9 us; of 256 17.2 and 12.6 us).
         LogprobsArgs b = a;
         auto go = [&](auto waves) {
             constexpr int W = decltype(waves)::value;

@@ -583,13 +583,29 @@ __global__ __launch_bounds__(VEC_BLOCK) void q4_quantize_kernel(const T *W, int6
 
 }  // namespace
 
-// Which kernel serves a call, by its sizes and types alone; figures are for bfloat16 rows and groups of 32 on 256 compute
-// units.
-//   Few rows, one register in four (up to 4 rows), two (8) or all: a wave per tile and stretch of the features while the
-//   tiles are few (4096 x 4096, one row: 4.7 us, four tiles a wave 8.3 us), four tiles a wave, which read the rows' operands
-//   once, when there are many (8192 x 65536: 57 us, one tile a wave 80 us).
-//   More rows: the largest tile that still gives most compute units a workgroup (256 rows, 4096 x 32768 in groups of 128:
-//   128 rows x 256 classes 64 us, 32 x 128 115 us; 128 rows, 4096 x 8192: 32 x 128 21 us, 128 x 256 64 us).
+// Which kernel serves a call, by its sizes and types alone.  Figures: 4096 features, groups of 32 (64 for 5 to 8 float rows) on
+// 256 compute units, in us, bfloat16 rows unless float is said; a tile is 16 classes.
+//   Few rows take one register in four (up to 4 rows), two (8) or all (16).  Few tiles: one or two a workgroup, so that every
+//   compute unit has one.  Many: four a workgroup, which read the rows' operands once.  The border lies where the small
+//   workgroups begin to take another turn on the chip; splitting float rows is worth sharing sooner.
+//     1 row    one tile / four     8192 classes 5.8 / 8.3    20480 10.3 / 10.9   32768 14.7 / 13.6   65536 34.8 / 26.4
+//     4 float  one / four          8192  8.5 / 9.6           12288 12.0 / 10.9   14336 14.2 / 11.3   65536 53.5 / 33.6
+//     8        two / four          8192  7.6 / 8.8           16384 11.6 / 10.1   20480 14.3 / 12.4 (1024 features: 4.9 / 5.2)
+//     5 float  two / four by eight waves / four by four waves
+//              8192 8.6 / 10.0 / 14.1    12288 11.4 / 11.2 / 14.8    24576 17.8 / 16.1 / 17.4    65536 42.8 / 34.2 / 32.3
+//              (in groups of 32: 45.4 / 45.5 / 39.2)
+//     16       two / four          8192  8.5 / 10.4          12288 12.5 / 10.8   24576 17.9 / 16.1
+//     16 float two / four / tile kernel  8192 14.2 / 16.5 / 17.6   12288 24.6 / 16.7 / 18.0   16384 25.8 / 17.4 / 19.2   24576 36.3 / 30.2 / 21.3
+//   More float rows: 16 rows by 128 classes, by eight waves (four groups of features) while that makes less than two workgroups
+//   a compute unit, by four beyond: 32 rows, 16384 classes 22.9 / 28.1, 32768 43.9 / 40.4, 131072 181 / 150.
+//   More 16-bit rows: the largest tile that still gives 5/8 of the compute units a workgroup,
+//     32 rows   16 x 128 / 32 x 128       16384 classes 18.4 / 18.4   20480 22.0 / 18.7    32768 30.0 / 23.0
+//     64        32 x 128 / 64 x 128       16384 21.6 / 29.5           20480 35.4 / 30.1    32768 41.1 / 30.9
+//     64        64 x 128 / 64 x 256       32768 30.9 / 40.8           40960 56.5 / 41.7    65536 65.4 / 51.3
+//     128       64 x 256 / 128 x 256      32768 46.3 / 74.1           40960 82.5 / 74.9    65536 100 / 86.7
+//   So few classes that most compute units would have nothing: parts of the features, each with 64 blocks (few rows) or 32,
+//   joined by a launch of its own (20000 features, 1000 classes, 1 row: one part 10.8, two 9.1, four 7.6; 64 rows: one 51, four
+//   20.0, eight 17.4; 8192 features, 1 row: one 4.9, two 5.8).
 namespace {
 enum Q4Form : int {
     Q4_ROWS4, Q4_ROWS4_WIDE, Q4_ROWS8, Q4_ROWS8_SPLIT, Q4_ROWS8_WIDE, Q4_ROWS16, Q4_ROWS16_WIDE,       // stream kernel
@@ -607,11 +623,10 @@ void q4_plan(int num_cus, Q4Args *a)
         a->form = tiles >= (split ? 7 : 10) * num_cus / 2 ? Q4_ROWS4_WIDE : Q4_ROWS4;
         groups = a->form == Q4_ROWS4 ? tiles : tiles / 4;
     } else if (n <= 8) {
-        // splitting fp32 rows is worth four tiles sooner (5 rows, 5003 x 10007: 13.5 us, two tiles 15.0 us)
-        a->form = tiles >= (split ? 6 : 5) * num_cus ? Q4_ROWS8_WIDE : split && tiles >= 2 * num_cus ? Q4_ROWS8_SPLIT : Q4_ROWS8;
+        a->form = tiles >= (split ? 6 : 5) * num_cus ? Q4_ROWS8_WIDE : split && tiles > 2 * num_cus ? Q4_ROWS8_SPLIT : Q4_ROWS8;
         groups = a->form == Q4_ROWS8 ? tiles / 2 + 1 : tiles / 4;
-    } else if (a->p < BLOCK || (n <= 16 && (!split || tiles < 4 * num_cus))) {
-        a->form = tiles >= (split ? 2 : 3) * num_cus ? Q4_ROWS16_WIDE : Q4_ROWS16;
+    } else if (a->p < BLOCK || (n <= 16 && (!split || tiles <= 4 * num_cus))) {
+        a->form = (split ? tiles > 2 * num_cus : tiles >= 3 * num_cus) ? Q4_ROWS16_WIDE : Q4_ROWS16;
         groups = (tiles / 2 + 1) * ((n + 15) / 16);
     } else if (split) {
         a->form = groups_of(n, K, 16, 128) >= 2 * num_cus ? Q4_TILE16_HALF : Q4_TILE16;
@@ -626,7 +641,6 @@ void q4_plan(int num_cus, Q4Args *a)
         groups = groups_of(n, K, 16, 128);
         share = 32;
     }
-    // so few classes that most compute units would have nothing: parts of the features, joined by a launch of its own
     int64_t parts = groups < num_cus / 2 ? num_cus / groups : 1;
     if (parts > blocks / share) parts = blocks / share;
     if (parts > 64) parts = 64;

@@ -59,6 +59,12 @@ def test_smallest_features(dtype, group, n, p, K):
         check(dtype, n, p, K, group, size, 1e30 if dtype != "f16" else 1e-4, n + 1)
 
 
+# float rows on both sides of the class counts where another form takes over (256 compute units)
+@pytest.mark.parametrize("n,K", [(6, 8192), (6, 8193), (12, 8192), (12, 8193), (16, 16384), (16, 16385), (4, 14336), (8, 24576)])
+def test_float_rows_at_the_borders(n, K):
+    check("f32", n, 300, K, 64, 1.0, 0.02, n)
+
+
 @pytest.mark.parametrize("dtype", list(F))
 def test_largest_scales(dtype):
     """The largest scales that there are, at features that make the margins finite, and classes whose codes are all zero."""
