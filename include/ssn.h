@@ -355,9 +355,9 @@ int ssn_logprobs_workspace(const ssn_rows *rows, int64_t *bytes);
  * Z, allowed and labels as in the forward call, logp, maxpart, logpart (and entropy if dentropy is given) its outputs;
  * dlogp [dev] n x m (NULL if m is 0), dlse, dentropy [dev, nullable] n, all of type A.  dZ [dev] like Z, leading dimension lddz: every
  * column of Z is written.  dZ may be Z itself (with lddz = ldz) and must not overlap it otherwise.
- * Classes that are not allowed and rows without a class get 0; a padding label and a given class of log
- * probability -inf contribute nothing; a row with NaN or +inf, or with a given class >= C, gets NaN at its allowed classes.  A class given
- * twice counts twice.  Returns like ssn_logprobs. */
+ * Classes that are not allowed, and all classes of a row without one of more than -inf, get 0; a padding label and a given
+ * class of log probability -inf contribute nothing; any other row with NaN or +inf, or with a given class >= C, gets NaN at its
+ * allowed classes.  A class given twice counts twice.  Returns like ssn_logprobs. */
 int ssn_logprobs_grad(const ssn_rows *rows, const void *logp, const void *maxpart, const void *logpart, const void *entropy,
                       const void *dlogp, const void *dlse, const void *dentropy, void *dZ, int64_t lddz);
 

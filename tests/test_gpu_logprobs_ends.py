@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_1802_09113_amd.binding import ssn_logprobs, ssn_logprobs_grad
 from tests.test_gpu_logprobs import DTYPES, check, some_labels
 
 pytestmark = pytest.mark.gpu
@@ -54,3 +55,17 @@ def test_alternatives_of_rows_full_of_ties_in_double(n, C):
     rng = np.random.default_rng(12)
     h = rng.integers(-3, 3, (n, C)).astype(np.float64)
     check(torch.from_numpy(h).cuda(), h, some_labels(n, 1, C, rng), min(64, C), False, None, grad=False)
+
+
+@pytest.mark.parametrize("C", [9, 300, 3000])
+def test_an_index_that_is_no_class_in_a_row_without_a_class(C):
+    """The row's gradient is zero, at its allowed classes too; in a row with a class it is NaN."""
+    Z = torch.randn(3, C, device="cuda")
+    Z[0] = -float("inf")
+    mask = torch.full((3, -(-C // 32)), -1, dtype=torch.int32, device="cuda")
+    mask[1] = 0
+    lab = torch.full((3, 2), C, dtype=torch.int32, device="cuda")
+    out = ssn_logprobs(Z, lab, allowed=mask)
+    assert bool(torch.isnan(out["logp"]).all())
+    dZ = ssn_logprobs_grad(Z, lab, out, dlogp=torch.ones(3, 2, device="cuda"), dlse=torch.ones(3, device="cuda"), allowed=mask)
+    assert bool((dZ[:2] == 0).all()) and bool(torch.isnan(dZ[2]).all())
