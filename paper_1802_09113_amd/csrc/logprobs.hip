@@ -9,9 +9,10 @@
 // left (the largest margin contributes e^0 = 1).  A lane may let its M lag a little behind (Gather), and takes back what its t
 // then holds too much before it is joined.  All of it in fp32 for fp32, fp16 and bf16 margins, in fp64 for fp64.
 //
-// What bounds it: memory on many long rows (8192 x 65536 bf16, one label: 179 us, 6.0 TB/s; the vector units are 60 % busy
-// with some nine instructions a margin), the vector units where a row is one workgroup's and alternatives are asked for, and
-// launch and latency on single rows (32000 fp32, five alternatives: 8.7 us a call, the kernel 6 to 9 us of it).
+// What bounds it: on many long rows the vector units (11 instructions a margin) as much as memory (8192 x 65536 bf16, one label: 181
+// to 187 us in a queue of passes, 5.7 to 5.9 TB/s; single launches in a trace 180 to 208).  Where a row is one workgroup's, the
+// vector units 60 % of the time and the first loads and last joins around that; launch and latency on single rows (32000 fp32, five
+// alternatives: 9.5 us a call, as the kernel alone).
 #include "ssn_internal.h"
 #include "ssn_math.h"
 
@@ -47,7 +48,7 @@ template <typename T> struct Vec {
     static constexpr int E = 16 / sizeof(T);
     typedef typename std::conditional<sizeof(T) == 2, RawAt2, RawAt4>::type RawAt;
     static __device__ __forceinline__ Raw load(const T *p) { return *(const RawAt *)p; }
-    // past the caches, which a gradient of any size worth a kernel outgrows: 8192 x 65536 bf16 367 -> 353 us, 1021 x 32003 fp32 57 -> 47 us
+    // past the caches, which a gradient of any size worth a kernel outgrows: 8192 x 65536 bf16 373 -> 355 us, 1021 x 32003 fp32 55 -> 51 us
     static __device__ __forceinline__ void store(T *p, Raw v) { __builtin_nontemporal_store(v, (RawAt *)p); }
 };
 

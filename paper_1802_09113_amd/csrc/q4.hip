@@ -16,9 +16,10 @@
 // share of the right operand of one 16x16x32 matrix instruction.  A wave reads the block with one load of 16 bytes per
 // lane; one, two or four matrix instructions in a row lie inside a group.
 //
-// What bounds it: for few rows the stream of codes and scales (one row, 8192 x 65536, groups of 32: 302 MB in 57 us, 5.3 TB/s),
-// for many the matrix cores (256 f16 rows, 4096 x 32768, groups of 128: 64 us, 1070 TFLOP/s, where a library product of
-// plain f16 matrices reaches 1160), and in groups of 32 the vector units that scale every group's sums (81 us).
+// What bounds it: for few rows the stream of codes and scales (one row, 8192 x 65536, groups of 32: 302 MB in 62 us in a queue of
+// passes, 4.9 TB/s, 57 us in a graph).  For many the matrix cores and the vector units, which convert codes and scale sums, in
+// turn, with two waves a SIMD (256 f16 rows, 4096 x 32768, groups of 128: 64 to 69 us, 1000 to 1070 TFLOP/s, where a library product
+// of plain f16 matrices reaches 1160; matrix cores 49 % busy, vector units 45 %), the more so in groups of 32 (84 to 87 us).
 #include "ssn_internal.h"
 
 #include <type_traits>
